@@ -18,6 +18,8 @@
  *     dare_lmhead_logprob     log-probability of given tokens (cross-entropy), logits never written either
  *     dare_lmhead_logprob_backward   its gradient with respect to the hidden states and the weights
  *     dare_attn_varlen        bidirectional attention over packed variable-length sequences
+ *     dare_qk_norm_rope (_backward)   norms of queries and keys per head with the position rotation, and their gradient
+ *     dare_paged_kv_append, dare_attn_paged   the same into a cache in pages, and one token's or a block's attention over it
  *     dare_forward_mask, dare_masked_nelbo   the forward (masking) process of Eq. 1 and the bound of Eq. 2
  *
  * Conventions
@@ -68,6 +70,7 @@ typedef enum {
 /* bits of the device status word */
 #define DARE_DEV_LEN_CLAMPED 1u   /* a prefix/suffix length exceeded its capacity and was clamped */
 #define DARE_DEV_WAIT_EXPIRED 2u  /* a bounded wait inside a kernel gave up; outputs are invalid  */
+#define DARE_DEV_INDEX_OUTSIDE 4u /* a position, sequence or page index lay outside its range: see the call */
 
 enum { DARE_SELECT_THRESHOLD = 0, DARE_SELECT_TOPK = 1 };
 
@@ -442,6 +445,60 @@ int dare_model_step_window(dare_model* model, int32_t* tokens, int B, int64_t ro
 int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_stride, int prompt_len, int gen_len,
                        int L, void* k_cache, void* v_cache, int cache_cap, int mode, float threshold, int k,
                        int32_t* pred, float* conf, int32_t* n_remaining, int32_t* steps_per_block, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------
+ * Norms of queries and keys per head, rotation, and a key-value cache in pages (rollouts of different lengths, prompts
+ * shared by several rollouts, sequences that are not at the same position).  The stacks behind block-diffusion rollouts
+ * (Section 3.4) normalise each query and key head before the rotation; dare_model_* does not, so these calls stand on
+ * their own, around a caller's projections (dare_linear).
+ *
+ * dare_rope_table: table fp32 [n_positions, d/2, 2] = (cos, sin)(position * base^(-2c/d)), evaluated in 64 bits; laid out once.
+ *
+ * dare_qk_norm_rope: row m of qkv bf16 [n_rows, (Hq + 2 Hkv) d] (q heads, k heads, v heads) at position positions[m]:
+ *     x <- x / sqrt(mean(x^2) + eps) * weight   for each q and k head (q_weight, k_weight bf16 [d]; both NULL: no norm)
+ *     (x_c, x_{c+d/2}) <- (x_c cos - x_{c+d/2} sin, x_{c+d/2} cos + x_c sin)
+ *   -> q_out bf16 [n_rows, Hq, d], k_out, v_out bf16 [n_rows, Hkv, d] (v copied); what dare_attn_varlen reads.  fp32 inside, rounded
+ *   once.  A position outside [0, n_positions) gives zeros and sets DARE_DEV_INDEX_OUTSIDE.
+ * dare_qk_norm_rope_backward: given the gradients d_q, d_k, d_v of those outputs, d_qkv bf16 (shape of qkv) and, with weights,
+ *   d_q_weight, d_k_weight fp32 [d] (sums over all rows and heads in a fixed order; without weights ignored).  A row that the forward
+ *   left at zero has a zero gradient.  Needs ctx workspace of 16 * d * (number of SMs) bytes with weights.
+ *
+ * The paged cache: k_pages, v_pages bf16 [n_pages, Hkv, page_size, d]; block_table int32 [n_seqs, max_pages]: position j of
+ * sequence b lives in page block_table[b, j / page_size] at index j % page_size.  Sequences may share pages.  page_size: a
+ * power of two from 16 to 1024; n_pages * Hkv * page_size < 2^31 - 1024; max_pages * page_size <= 2^30.
+ *
+ * dare_paged_kv_append: the arithmetic of dare_qk_norm_rope; q goes to q_out [n_rows, Hq, d], k and v to position positions[m] of
+ *   sequence seq_ids[m].  A row with seq_ids[m] < 0 belongs to no sequence: nothing is read or written for it (a padded
+ *   batch).  A sequence >= n_seqs, a position outside [0, min(n_positions, max_pages * page_size)) or a page outside [0, n_pages): the row is left
+ *   out, q_out included, and DARE_DEV_INDEX_OUTSIDE is set.  Each position of the cache at most once per call.
+ *
+ * dare_attn_paged: the last L positions of each sequence attend to it: n = kv_lens[b] keys, the L new ones (appended before)
+ *   among them; query i of q bf16 [B, L, Hq, d] stands at position n - L + i.
+ *     o = softmax_j(scale <q, k_j>) v_j over j < n with  window = 0  or  j < sinks  or  j > n - L + i - window
+ *   (bidirectional inside the block, as dare_attn_block; L = 1 is the single token).  out bf16 [B, L, Hq, d]; lse fp32 [B, Hq, L] or
+ *   NULL; scale 0 => 1/sqrt(d).  Nothing visible (n = 0): out = 0, lse = -inf.  n beyond max_pages * page_size is clamped
+ *   (DARE_DEV_LEN_CLAMPED).  Pages that no query of the block can see, those between the sinks and the window and those
+ *   behind n, are not read and their table entries may be anything; a page outside [0, n_pages) that one can see reads as zeros and
+ *   sets DARE_DEV_INDEX_OUTSIDE.  Cached values that some query of a block sees must be finite for all of its queries.
+ *   Results do not depend on the order in which the GPU runs the parts.  Supported: Hq % Hkv == 0, d in {64, 128}, L >= 1,
+ *   L * Hq / Hkv <= 2^20; ctx workspace of 1024 * (d + 2) bytes for each SM.
+ */
+int dare_rope_table(dare_ctx* ctx, int n_positions, int d, double base, float* table, void* stream);
+int dare_qk_norm_rope(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight, const void* k_weight,
+                      float eps, const int32_t* positions, const float* rope_table, int n_positions, void* q_out, void* k_out,
+                      void* v_out, void* stream);
+int dare_qk_norm_rope_backward(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight,
+                               const void* k_weight, float eps, const int32_t* positions, const float* rope_table, int n_positions,
+                               const void* d_q, const void* d_k, const void* d_v, void* d_qkv, float* d_q_weight,
+                               float* d_k_weight, void* stream);
+int dare_paged_kv_append(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight,
+                         const void* k_weight, float eps, const float* rope_table, int n_positions, const int32_t* seq_ids,
+                         const int32_t* positions, const int32_t* block_table, int n_seqs, int max_pages, int n_pages, int page_size,
+                         void* k_pages, void* v_pages, void* q_out, void* stream);
+int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int d, float scale, const void* q, const void* k_pages,
+                    const void* v_pages, int n_pages, int page_size, const int32_t* block_table, int max_pages,
+                    const int32_t* kv_lens, int window, int sinks, void* out, float* lse, void* stream);
 
 /*
  * Allocation-free variant of dare_lmhead_confidence.  (The paper has no counterpart for this entry

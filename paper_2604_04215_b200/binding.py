@@ -24,13 +24,15 @@ SELECT_THRESHOLD = 0
 SELECT_TOPK = 1
 DEV_LEN_CLAMPED = 1
 DEV_WAIT_EXPIRED = 2
+DEV_INDEX_OUTSIDE = 4
 
 EXPORTS = ["dare_create", "dare_destroy", "dare_status_string", "dare_device_status", "dare_sm_count",
            "dare_tmap_cache_stats", "dare_lmhead_static_status", "dare_kernel_launches",
            "dare_attn_block", "dare_attn_varlen", "dare_lmhead_confidence", "dare_unmask_select", "dare_denoise_block", "dare_denoise_block_sampled",
            "dare_lmhead_confidence_static", "dare_lmhead_sample", "dare_lmhead_logprob", "dare_lmhead_logprob_backward", "dare_transpose_bf16", "dare_forward_mask", "dare_masked_nelbo", "dare_model_create", "dare_model_destroy", "dare_model_forward",
            "dare_model_step", "dare_generate", "dare_model_set_sampling", "dare_model_forward_window", "dare_model_step_window", "dare_generate_dual",
-           "dare_linear", "dare_linear_plan", "dare_rmsnorm", "dare_rope_kv_write"]
+           "dare_linear", "dare_linear_plan", "dare_rmsnorm", "dare_rope_kv_write",
+           "dare_rope_table", "dare_qk_norm_rope", "dare_qk_norm_rope_backward", "dare_paged_kv_append", "dare_attn_paged"]
 
 _lib = None
 _marshal = None
@@ -128,6 +130,16 @@ def load():
     lib.dare_rmsnorm.restype = i32
     lib.dare_rope_kv_write.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, i32, vp]
     lib.dare_rope_kv_write.restype = i32
+    lib.dare_rope_table.argtypes = [vp, i32, i32, C.c_double, vp, vp]
+    lib.dare_rope_table.restype = i32
+    lib.dare_qk_norm_rope.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, f32, vp, vp, i32, vp, vp, vp, vp]
+    lib.dare_qk_norm_rope.restype = i32
+    lib.dare_qk_norm_rope_backward.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, f32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.dare_qk_norm_rope_backward.restype = i32
+    lib.dare_paged_kv_append.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, f32, vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.dare_paged_kv_append.restype = i32
+    lib.dare_attn_paged.argtypes = [vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, i32, i32, vp, i32, vp, i32, i32, vp, vp, vp]
+    lib.dare_attn_paged.restype = i32
     _lib = lib
     return lib
 
@@ -205,7 +217,7 @@ class _NoNative:
     def _none(*args):
         return None
 
-    denoise_block = denoise_block_sampled = attn_varlen = _none
+    denoise_block = denoise_block_sampled = attn_varlen = attn_paged = paged_kv_append = qk_norm_rope = qk_norm_rope_backward = _none
 
 
 def _native():
@@ -712,3 +724,148 @@ def dare_model_set_sampling(model: Model, temperature: float, seed: int = 0, fir
     if rc != 0 and check:
         raise DareError(rc, "dare_model_set_sampling")
     return rc
+
+
+def _same(name: str, t, *shape):
+    """Sizes that are not handed to the library with a tensor have to agree with those that are."""
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+
+
+def _fused_heads(cols: int, n_kv_heads: int, d: int) -> int:
+    """Query heads of a fused projection's row [(Hq + 2 Hkv) d]."""
+    hq = cols // d - 2 * n_kv_heads
+    if hq < 1 or cols % d:
+        raise ValueError(f"rows of {cols} values do not hold {n_kv_heads} key and value heads of {d} and a query head")
+    return hq
+
+
+def dare_rope_table(ctx: Context, n_positions: int, head_dim: int, base: float = 10000.0, table=None, stream=None,
+                    check: bool = True):
+    """fp32 [n_positions, head_dim / 2, 2]: (cos, sin) of position * base^(-2c/d)."""
+    if table is None:
+        table = torch.empty(n_positions, head_dim // 2, 2, dtype=torch.float32, device="cuda")
+    _same("table", table, n_positions, head_dim // 2, 2)
+    rc = load().dare_rope_table(ctx.handle, int(n_positions), int(head_dim), float(base), _ptr(table, torch.float32), _stream(stream))
+    if rc != 0 and check:
+        raise DareError(rc, "dare_rope_table")
+    return table if check else rc
+
+
+def dare_qk_norm_rope(ctx: Context, qkv, positions, rope_table, n_kv_heads: int, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      q_out=None, k_out=None, v_out=None, stream=None, check: bool = True):
+    """Norms of q and k per head, rotation: (q [rows, Hq, d], k [rows, Hkv, d], v [rows, Hkv, d])."""
+    rows, d, hkv = qkv.shape[0], 2 * rope_table.shape[1], int(n_kv_heads)
+    hq = _fused_heads(qkv.shape[1], hkv, d)
+    bf, dev = torch.bfloat16, torch.cuda.current_device()
+    q_out = torch.empty(rows, hq, d, dtype=bf, device=qkv.device) if q_out is None else q_out
+    k_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if k_out is None else k_out
+    v_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if v_out is None else v_out
+    rc = _native().qk_norm_rope(ctx.handle.value, dev, _raw(stream, dev), qkv, positions, rope_table, q_weight, k_weight, eps, q_out,
+                                k_out, v_out)
+    if rc is None:
+        _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
+        _same("positions", positions, rows)
+        _same("rope_table", rope_table, rope_table.shape[0], d // 2, 2)
+        _same("q_weight", q_weight, d)
+        _same("k_weight", k_weight, d)
+        _same("q_out", q_out, rows, hq, d)
+        _same("k_out", k_out, rows, hkv, d)
+        _same("v_out", v_out, rows, hkv, d)
+        rc = load().dare_qk_norm_rope(ctx.handle, _addr(qkv, bf, dev), rows, hq, hkv, d, _addr(q_weight, bf, dev), _addr(k_weight, bf, dev),
+                                      float(eps), _addr(positions, torch.int32, dev), _addr(rope_table, torch.float32, dev),
+                                      rope_table.shape[0], _addr(q_out, bf, dev), _addr(k_out, bf, dev), _addr(v_out, bf, dev),
+                                      _stream(stream, dev))
+    if rc != 0 and check:
+        raise DareError(rc, "dare_qk_norm_rope")
+    return (q_out, k_out, v_out) if check else rc
+
+
+def dare_qk_norm_rope_backward(ctx: Context, qkv, positions, rope_table, d_q, d_k, d_v, q_weight=None, k_weight=None, eps: float = 1e-6,
+                               d_qkv=None, d_q_weight=None, d_k_weight=None, stream=None, check: bool = True):
+    """Gradient of dare_qk_norm_rope: (d_qkv, d_q_weight, d_k_weight); the last two None without weights."""
+    rows, hq, d = d_q.shape
+    hkv = d_k.shape[1]
+    bf, f32, dev = torch.bfloat16, torch.float32, torch.cuda.current_device()
+    d_qkv = torch.empty_like(qkv) if d_qkv is None else d_qkv
+    if q_weight is None:
+        d_q_weight = d_k_weight = None
+    else:
+        d_q_weight = torch.empty(d, dtype=f32, device=qkv.device) if d_q_weight is None else d_q_weight
+        d_k_weight = torch.empty(d, dtype=f32, device=qkv.device) if d_k_weight is None else d_k_weight
+    rc = _native().qk_norm_rope_backward(ctx.handle.value, dev, _raw(stream, dev), qkv, positions, rope_table, d_q, d_k, d_v, q_weight,
+                                         k_weight, eps, d_qkv, d_q_weight, d_k_weight)
+    if rc is None:
+        _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
+        _same("positions", positions, rows)
+        _same("rope_table", rope_table, rope_table.shape[0], d // 2, 2)
+        _same("d_k", d_k, rows, hkv, d)
+        _same("d_v", d_v, rows, hkv, d)
+        _same("d_qkv", d_qkv, rows, (hq + 2 * hkv) * d)
+        for name, t in (("q_weight", q_weight), ("k_weight", k_weight), ("d_q_weight", d_q_weight), ("d_k_weight", d_k_weight)):
+            _same(name, t, d)
+        rc = load().dare_qk_norm_rope_backward(
+            ctx.handle, _addr(qkv, bf, dev), rows, hq, hkv, d, _addr(q_weight, bf, dev), _addr(k_weight, bf, dev), float(eps),
+            _addr(positions, torch.int32, dev), _addr(rope_table, f32, dev), rope_table.shape[0], _addr(d_q, bf, dev), _addr(d_k, bf, dev),
+            _addr(d_v, bf, dev), _addr(d_qkv, bf, dev), _addr(d_q_weight, f32, dev), _addr(d_k_weight, f32, dev), _stream(stream, dev))
+    if rc != 0 and check:
+        raise DareError(rc, "dare_qk_norm_rope_backward")
+    return (d_qkv, d_q_weight, d_k_weight) if check else rc
+
+
+def dare_paged_kv_append(ctx: Context, qkv, seq_ids, positions, block_table, k_pages, v_pages, rope_table, q_weight=None, k_weight=None,
+                         eps: float = 1e-6, q_out=None, stream=None, check: bool = True):
+    """Norms of q and k per head, rotation, k and v into their pages; returns q [rows, Hq, d].  Rows with seq_ids < 0 are left out."""
+    n_pages, hkv, page, d = k_pages.shape
+    rows = qkv.shape[0]
+    hq = _fused_heads(qkv.shape[1], hkv, d)
+    bf, i32, dev = torch.bfloat16, torch.int32, torch.cuda.current_device()
+    if q_out is None:
+        q_out = torch.empty(rows, hq, d, dtype=bf, device=qkv.device)
+    rc = _native().paged_kv_append(ctx.handle.value, dev, _raw(stream, dev), qkv, seq_ids, positions, block_table, k_pages, v_pages,
+                                   rope_table, q_weight, k_weight, eps, q_out)
+    if rc is None:
+        _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
+        _same("seq_ids", seq_ids, rows)
+        _same("positions", positions, rows)
+        _same("block_table", block_table, *block_table.shape[:2])
+        _same("v_pages", v_pages, n_pages, hkv, page, d)
+        _same("rope_table", rope_table, rope_table.shape[0], d // 2, 2)
+        _same("q_weight", q_weight, d)
+        _same("k_weight", k_weight, d)
+        _same("q_out", q_out, rows, hq, d)
+        rc = load().dare_paged_kv_append(
+            ctx.handle, _addr(qkv, bf, dev), rows, hq, hkv, d, _addr(q_weight, bf, dev), _addr(k_weight, bf, dev), float(eps),
+            _addr(rope_table, torch.float32, dev), rope_table.shape[0], _addr(seq_ids, i32, dev), _addr(positions, i32, dev),
+            _addr(block_table, i32, dev), block_table.shape[0], block_table.shape[1], n_pages, page, _addr(k_pages, bf, dev),
+            _addr(v_pages, bf, dev), _addr(q_out, bf, dev), _stream(stream, dev))
+    if rc != 0 and check:
+        raise DareError(rc, "dare_paged_kv_append")
+    return q_out if check else rc
+
+
+def dare_attn_paged(ctx: Context, q, k_pages, v_pages, block_table, kv_lens, window: int = 0, sinks: int = 0, out=None, lse=None,
+                    scale: float = 0.0, stream=None, check: bool = True):
+    """The last L positions of each sequence, q [B, L, Hq, d], over its pages."""
+    if out is None:
+        out = torch.empty_like(q)
+    dev = torch.cuda.current_device()
+    rc = _native().attn_paged(ctx.handle.value, dev, _raw(stream, dev), scale, q, k_pages, v_pages, block_table, kv_lens, window, sinks,
+                              out, lse)
+    if rc is None:
+        B, L, hq, d = q.shape
+        n_pages, hkv, page, _ = k_pages.shape
+        bf, i32 = torch.bfloat16, torch.int32
+        _same("k_pages", k_pages, n_pages, hkv, page, d)
+        _same("v_pages", v_pages, n_pages, hkv, page, d)
+        _same("block_table", block_table, B, block_table.shape[1])
+        _same("kv_lens", kv_lens, B)
+        _same("out", out, B, L, hq, d)
+        _same("lse", lse, B, hq, L)
+        rc = load().dare_attn_paged(
+            ctx.handle, B, L, hq, hkv, d, float(scale), _addr(q, bf, dev), _addr(k_pages, bf, dev), _addr(v_pages, bf, dev), n_pages, page,
+            _addr(block_table, i32, dev), block_table.shape[1], _addr(kv_lens, i32, dev), int(window), int(sinks), _addr(out, bf, dev),
+            _addr(lse, torch.float32, dev), _stream(stream, dev))
+    if rc != 0 and check:
+        raise DareError(rc, "dare_attn_paged")
+    return out if check else rc

@@ -138,6 +138,7 @@ int dare_create(dare_ctx** out, int device, size_t workspace_bytes) {
     ctx->workspace_bytes = workspace_bytes ? workspace_bytes : (size_t(256) << 20);
     ctx->workspace = nullptr;
     ctx->dev_status = nullptr;
+    ctx->join_counters = nullptr;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess ||
@@ -149,9 +150,12 @@ int dare_create(dare_ctx** out, int device, size_t workspace_bytes) {
     ctx->encode_tiled = reinterpret_cast<dare_encode_tiled_fn>(fn);
     if (cudaMalloc(&ctx->workspace, ctx->workspace_bytes) != cudaSuccess ||
         cudaMalloc(reinterpret_cast<void**>(&ctx->dev_status), sizeof(uint32_t)) != cudaSuccess ||
-        cudaMemset(ctx->dev_status, 0, sizeof(uint32_t)) != cudaSuccess) {
+        cudaMemset(ctx->dev_status, 0, sizeof(uint32_t)) != cudaSuccess ||
+        cudaMalloc(reinterpret_cast<void**>(&ctx->join_counters), dare::PAGED_MAX_CTAS * sizeof(uint32_t)) != cudaSuccess ||
+        cudaMemset(ctx->join_counters, 0, dare::PAGED_MAX_CTAS * sizeof(uint32_t)) != cudaSuccess) {
         if (ctx->workspace) cudaFree(ctx->workspace);
         if (ctx->dev_status) cudaFree(ctx->dev_status);
+        if (ctx->join_counters) cudaFree(ctx->join_counters);
         delete ctx->tmaps;
         delete ctx;
         return DARE_ERR_CUDA;
@@ -165,6 +169,7 @@ int dare_destroy(dare_ctx* ctx) {
     dare::DeviceScope scope(ctx->device);
     cudaFree(ctx->workspace);
     cudaFree(ctx->dev_status);
+    cudaFree(ctx->join_counters);
     delete ctx->tmaps;
     delete ctx;
     return DARE_OK;
@@ -200,6 +205,11 @@ int dare_device_status(dare_ctx* ctx, void* stream, uint32_t* host_out) {
         return DARE_ERR_CUDA;
     if (cudaMemsetAsync(ctx->dev_status, 0, sizeof(uint32_t), s) != cudaSuccess) return DARE_ERR_CUDA;
     if (cudaStreamSynchronize(s) != cudaSuccess) return DARE_ERR_CUDA;
+    // a launch that gave up may have left its counts of joined parts behind
+    if ((*host_out & DARE_DEV_WAIT_EXPIRED) &&
+        (cudaMemsetAsync(ctx->join_counters, 0, dare::PAGED_MAX_CTAS * sizeof(uint32_t), s) != cudaSuccess ||
+         cudaStreamSynchronize(s) != cudaSuccess))
+        return DARE_ERR_CUDA;
     return DARE_OK;
 }
 

@@ -37,6 +37,7 @@ struct dare_ctx {
     void* workspace;
     size_t workspace_bytes;
     uint32_t* dev_status;   // device word, bits DARE_DEV_*
+    uint32_t* join_counters;  // PAGED_MAX_CTAS device words, 0 between calls (paged.cu)
     dare_encode_tiled_fn encode_tiled;
     TmapCache* tmaps;       // host memory; NULL = encode on every call
 };
@@ -131,6 +132,19 @@ inline int check_current_device(const dare_ctx* ctx) {
     return dev == ctx->device ? DARE_OK : DARE_ERR_DEVICE;
 }
 
+// A paged cache [n_pages, Hkv, page_size, d] and the table [n_seqs, max_pages] of its sequences.  Rows of the pool are TMA
+// coordinates and positions 32-bit integers; a page is a power of two of at least 16 positions (a row index is a shift and a
+// mask, and a page's rows keep the 8-row pattern of the 128-byte swizzle).
+inline int check_pages(int n_seqs, int max_pages, int n_pages, int page_size, int Hkv) {
+    if (n_seqs < 1 || max_pages < 1 || n_pages < 1 || page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)))
+        return DARE_ERR_SHAPE;
+    if (static_cast<long long>(max_pages) * page_size > (1LL << 30)) return DARE_ERR_SHAPE;
+    if (static_cast<long long>(n_pages) * page_size > (0x7fffffffLL - 1024) / Hkv) return DARE_ERR_SHAPE;
+    return DARE_OK;
+}
+// CTAs (and join counters) of an attention launch over a paged cache, at most.
+constexpr int PAGED_MAX_CTAS = 1024;
+
 // bf16 2-D row-major tensor [rows, cols] -> tensor map with a [box_rows, 64] box and 128-byte swizzle.
 int make_tmap_bf16_2d(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols,
                       uint32_t box_rows, uint32_t box_cols);
@@ -219,7 +233,7 @@ int gemm_plan_describe(const dare_ctx* ctx, int epi, int M, int N, int K, int* o
 int launch_embed(const void* emb, int D, int V, const int32_t* tokens, int64_t row_stride, int start, int length,
                  int n_rows, void* x, cudaStream_t stream);
 int launch_rmsnorm(const void* x, int D, int n_rows, float eps, void* y, int sm_count, cudaStream_t stream);
-// cs [n_pos][half] and cs_t [half][n_pos]: (cos, sin) pairs
+// cs [n_pos][half] and cs_t [half][n_pos] (or NULL): (cos, sin) pairs
 int launch_rope_table(float* cs, float* cs_t, int n_pos, int half, double base, cudaStream_t stream);
 int launch_rope_kv_write(const void* qkv, int n_rows, int Hq, int Hkv, int d, int start, int length, const float* cs,
                          void* q_out, void* k_cache, void* v_cache, int cap, int sm_count, cudaStream_t stream);

@@ -116,7 +116,7 @@ rmsnorm_warp_kernel(const uint4* __restrict__ x, int D8, int n_rows, float eps, 
     }
 }
 
-// cs[p, c] = (cos, sin)(p * base^(-2c/d)), c < d/2, evaluated in double precision; cs_t is its transpose.
+// cs[p, c] = (cos, sin)(p * base^(-2c/d)), c < d/2, evaluated in double precision; cs_t (or NULL) is its transpose.
 __global__ void rope_table_kernel(float2* __restrict__ cs, float2* __restrict__ cs_t, int n_pos, int half, double base) {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     pdl_wait();
@@ -126,7 +126,7 @@ __global__ void rope_table_kernel(float2* __restrict__ cs, float2* __restrict__ 
     double s, co;
     sincos(ang, &s, &co);
     cs[i] = make_float2(static_cast<float>(co), static_cast<float>(s));
-    cs_t[static_cast<size_t>(c) * n_pos + p] = cs[i];
+    if (cs_t != nullptr) cs_t[static_cast<size_t>(c) * n_pos + p] = cs[i];
 }
 
 // Row m = (b, i) of the fused QKV projection [n_rows, (Hq + 2 Hkv) d], position p = start + i:

@@ -17,6 +17,10 @@ namespace {
 decltype(&dare_denoise_block) f_denoise = nullptr;
 decltype(&dare_denoise_block_sampled) f_denoise_sampled = nullptr;
 decltype(&dare_attn_varlen) f_varlen = nullptr;
+decltype(&dare_attn_paged) f_attn_paged = nullptr;
+decltype(&dare_paged_kv_append) f_paged_append = nullptr;
+decltype(&dare_qk_norm_rope) f_qk_norm = nullptr;
+decltype(&dare_qk_norm_rope_backward) f_qk_norm_back = nullptr;
 
 // Walks the argument list; `ok` turns false at the first argument that does not fit.
 struct Args {
@@ -164,6 +168,137 @@ PyObject* varlen_checked(PyObject* const* argv, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
+// Whether a tensor has this shape (NULL: an argument that was left out).
+bool has_shape(const at::Tensor* t, std::initializer_list<int64_t> shape) { return !t || t->sizes() == at::IntArrayRef(shape); }
+const void* data_of(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+int as_int(int64_t x) { return x >= 0 && x <= 0x7fffffff ? static_cast<int>(x) : -1; }      // (the library refuses -1)
+
+// (handle, device, stream, scale, q, k_pages, v_pages, block_table, kv_lens, window, sinks, out, lse)
+PyObject* attn_paged_checked(PyObject* const* argv, Py_ssize_t n) {
+    Args a{argv, n};
+    dare_ctx* ctx = static_cast<dare_ctx*>(a.address());
+    a.device = static_cast<long>(a.integer());
+    void* stream = a.address();
+    const float scale = static_cast<float>(a.real());
+    const at::Tensor *q = a.tensor(at::kBFloat16), *k = a.tensor(at::kBFloat16), *v = a.tensor(at::kBFloat16);
+    const at::Tensor *table = a.tensor(at::kInt), *lens = a.tensor(at::kInt);
+    const long long window = a.integer(), sinks = a.integer();
+    const at::Tensor *out = a.tensor(at::kBFloat16), *lse = a.tensor(at::kFloat);
+    if (!a.ok || a.at != n || !q || !k || !v || !table || !lens || !out || q->dim() != 4 || k->dim() != 4 || table->dim() != 2) Py_RETURN_NONE;
+    if (window != static_cast<int>(window) || sinks != static_cast<int>(sinks)) Py_RETURN_NONE;
+    const int64_t B = q->size(0), L = q->size(1), Hq = q->size(2), d = q->size(3);
+    if (k->size(3) != d || v->sizes() != k->sizes() || out->sizes() != q->sizes() || table->size(0) != B || !has_shape(lens, {B}) ||
+        !has_shape(lse, {B, Hq, L}))
+        Py_RETURN_NONE;
+    const void *q_ptr = q->data_ptr(), *k_ptr = k->data_ptr(), *v_ptr = v->data_ptr();
+    const int32_t *t_ptr = static_cast<const int32_t*>(table->data_ptr()), *n_ptr = static_cast<const int32_t*>(lens->data_ptr());
+    void* o_ptr = out->data_ptr();
+    float* l_ptr = static_cast<float*>(const_cast<void*>(data_of(lse)));
+    const int n_pages = as_int(k->size(0)), Hkv = as_int(k->size(1)), page = as_int(k->size(2)), max_pages = as_int(table->size(1));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = f_attn_paged(ctx, as_int(B), as_int(L), as_int(Hq), Hkv, as_int(d), scale, q_ptr, k_ptr, v_ptr, n_pages, page, t_ptr, max_pages, n_ptr,
+                      static_cast<int>(window), static_cast<int>(sinks), o_ptr, l_ptr, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (handle, device, stream, qkv, seq_ids, positions, block_table, k_pages, v_pages, rope_table, q_weight, k_weight, eps, q_out)
+PyObject* paged_append_checked(PyObject* const* argv, Py_ssize_t n) {
+    Args a{argv, n};
+    dare_ctx* ctx = static_cast<dare_ctx*>(a.address());
+    a.device = static_cast<long>(a.integer());
+    void* stream = a.address();
+    const at::Tensor *x = a.tensor(at::kBFloat16), *seq = a.tensor(at::kInt), *pos = a.tensor(at::kInt), *table = a.tensor(at::kInt);
+    const at::Tensor *k = a.tensor(at::kBFloat16), *v = a.tensor(at::kBFloat16), *rope = a.tensor(at::kFloat);
+    const at::Tensor *wq = a.tensor(at::kBFloat16), *wk = a.tensor(at::kBFloat16);
+    const float eps = static_cast<float>(a.real());
+    const at::Tensor* q = a.tensor(at::kBFloat16);
+    if (!a.ok || a.at != n || !x || !seq || !pos || !table || !k || !v || !rope || !q || x->dim() != 2 || k->dim() != 4 ||
+        table->dim() != 2 || rope->dim() != 3 || q->dim() != 3)
+        Py_RETURN_NONE;
+    const int64_t rows = x->size(0), Hkv = k->size(1), d = k->size(3), Hq = q->size(1);
+    if (!has_shape(x, {rows, (Hq + 2 * Hkv) * d}) || !has_shape(seq, {rows}) || !has_shape(pos, {rows}) || v->sizes() != k->sizes() ||
+        !has_shape(rope, {rope->size(0), d / 2, 2}) || !has_shape(wq, {d}) || !has_shape(wk, {d}) || !has_shape(q, {rows, Hq, d}))
+        Py_RETURN_NONE;
+    const void *x_ptr = x->data_ptr(), *wq_ptr = data_of(wq), *wk_ptr = data_of(wk);
+    const float* r_ptr = static_cast<const float*>(rope->data_ptr());
+    const int32_t *s_ptr = static_cast<const int32_t*>(seq->data_ptr()), *p_ptr = static_cast<const int32_t*>(pos->data_ptr());
+    const int32_t* t_ptr = static_cast<const int32_t*>(table->data_ptr());
+    void *k_ptr = k->data_ptr(), *v_ptr = v->data_ptr(), *q_ptr = q->data_ptr();
+    const int n_pos = as_int(rope->size(0)), n_seqs = as_int(table->size(0)), max_pages = as_int(table->size(1));
+    const int n_pages = as_int(k->size(0)), page = as_int(k->size(2));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = f_paged_append(ctx, x_ptr, as_int(rows), as_int(Hq), as_int(Hkv), as_int(d), wq_ptr, wk_ptr, eps, r_ptr, n_pos, s_ptr, p_ptr, t_ptr,
+                        n_seqs, max_pages, n_pages, page, k_ptr, v_ptr, q_ptr, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (handle, device, stream, qkv, positions, rope_table, q_weight, k_weight, eps, q_out, k_out, v_out)
+PyObject* qk_norm_checked(PyObject* const* argv, Py_ssize_t n) {
+    Args a{argv, n};
+    dare_ctx* ctx = static_cast<dare_ctx*>(a.address());
+    a.device = static_cast<long>(a.integer());
+    void* stream = a.address();
+    const at::Tensor *x = a.tensor(at::kBFloat16), *pos = a.tensor(at::kInt), *rope = a.tensor(at::kFloat);
+    const at::Tensor *wq = a.tensor(at::kBFloat16), *wk = a.tensor(at::kBFloat16);
+    const float eps = static_cast<float>(a.real());
+    const at::Tensor *q = a.tensor(at::kBFloat16), *k = a.tensor(at::kBFloat16), *v = a.tensor(at::kBFloat16);
+    if (!a.ok || a.at != n || !x || !pos || !rope || !q || !k || !v || x->dim() != 2 || rope->dim() != 3 || q->dim() != 3 || k->dim() != 3)
+        Py_RETURN_NONE;
+    const int64_t rows = x->size(0), Hq = q->size(1), Hkv = k->size(1), d = q->size(2);
+    if (!has_shape(x, {rows, (Hq + 2 * Hkv) * d}) || !has_shape(pos, {rows}) || !has_shape(rope, {rope->size(0), d / 2, 2}) ||
+        !has_shape(wq, {d}) || !has_shape(wk, {d}) || !has_shape(q, {rows, Hq, d}) || !has_shape(k, {rows, Hkv, d}) || !has_shape(v, {rows, Hkv, d}))
+        Py_RETURN_NONE;
+    const void *x_ptr = x->data_ptr(), *wq_ptr = data_of(wq), *wk_ptr = data_of(wk);
+    const float* r_ptr = static_cast<const float*>(rope->data_ptr());
+    const int32_t* p_ptr = static_cast<const int32_t*>(pos->data_ptr());
+    void *q_ptr = q->data_ptr(), *k_ptr = k->data_ptr(), *v_ptr = v->data_ptr();
+    const int n_pos = as_int(rope->size(0));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = f_qk_norm(ctx, x_ptr, as_int(rows), as_int(Hq), as_int(Hkv), as_int(d), wq_ptr, wk_ptr, eps, p_ptr, r_ptr, n_pos, q_ptr, k_ptr, v_ptr,
+                   stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
+// (handle, device, stream, qkv, positions, rope_table, d_q, d_k, d_v, q_weight, k_weight, eps, d_qkv, d_q_weight, d_k_weight)
+PyObject* qk_norm_back_checked(PyObject* const* argv, Py_ssize_t n) {
+    Args a{argv, n};
+    dare_ctx* ctx = static_cast<dare_ctx*>(a.address());
+    a.device = static_cast<long>(a.integer());
+    void* stream = a.address();
+    const at::Tensor *x = a.tensor(at::kBFloat16), *pos = a.tensor(at::kInt), *rope = a.tensor(at::kFloat);
+    const at::Tensor *gq = a.tensor(at::kBFloat16), *gk = a.tensor(at::kBFloat16), *gv = a.tensor(at::kBFloat16);
+    const at::Tensor *wq = a.tensor(at::kBFloat16), *wk = a.tensor(at::kBFloat16);
+    const float eps = static_cast<float>(a.real());
+    const at::Tensor *dx = a.tensor(at::kBFloat16), *dwq = a.tensor(at::kFloat), *dwk = a.tensor(at::kFloat);
+    if (!a.ok || a.at != n || !x || !pos || !rope || !gq || !gk || !gv || !dx || x->dim() != 2 || rope->dim() != 3 || gq->dim() != 3 ||
+        gk->dim() != 3)
+        Py_RETURN_NONE;
+    const int64_t rows = x->size(0), Hq = gq->size(1), Hkv = gk->size(1), d = gq->size(2);
+    if (!has_shape(x, {rows, (Hq + 2 * Hkv) * d}) || !has_shape(pos, {rows}) || !has_shape(rope, {rope->size(0), d / 2, 2}) ||
+        !has_shape(wq, {d}) || !has_shape(wk, {d}) || !has_shape(dwq, {d}) || !has_shape(dwk, {d}) || !has_shape(gq, {rows, Hq, d}) ||
+        !has_shape(gk, {rows, Hkv, d}) || !has_shape(gv, {rows, Hkv, d}) || dx->sizes() != x->sizes())
+        Py_RETURN_NONE;
+    const void *x_ptr = x->data_ptr(), *wq_ptr = data_of(wq), *wk_ptr = data_of(wk);
+    const void *gq_ptr = gq->data_ptr(), *gk_ptr = gk->data_ptr(), *gv_ptr = gv->data_ptr();
+    const float* r_ptr = static_cast<const float*>(rope->data_ptr());
+    const int32_t* p_ptr = static_cast<const int32_t*>(pos->data_ptr());
+    void* dx_ptr = dx->data_ptr();
+    float *dwq_ptr = static_cast<float*>(const_cast<void*>(data_of(dwq))), *dwk_ptr = static_cast<float*>(const_cast<void*>(data_of(dwk)));
+    const int n_pos = as_int(rope->size(0));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = f_qk_norm_back(ctx, x_ptr, as_int(rows), as_int(Hq), as_int(Hkv), as_int(d), wq_ptr, wk_ptr, eps, p_ptr, r_ptr, n_pos, gq_ptr, gk_ptr,
+                        gv_ptr, dx_ptr, dwq_ptr, dwk_ptr, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+
 template <PyObject* (*CALL)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     try {
@@ -183,8 +318,12 @@ PyObject* bind(PyObject*, PyObject* arg) {
         f_denoise = reinterpret_cast<decltype(f_denoise)>(dlsym(lib, "dare_denoise_block"));
         f_denoise_sampled = reinterpret_cast<decltype(f_denoise_sampled)>(dlsym(lib, "dare_denoise_block_sampled"));
         f_varlen = reinterpret_cast<decltype(f_varlen)>(dlsym(lib, "dare_attn_varlen"));
+        f_attn_paged = reinterpret_cast<decltype(f_attn_paged)>(dlsym(lib, "dare_attn_paged"));
+        f_paged_append = reinterpret_cast<decltype(f_paged_append)>(dlsym(lib, "dare_paged_kv_append"));
+        f_qk_norm = reinterpret_cast<decltype(f_qk_norm)>(dlsym(lib, "dare_qk_norm_rope"));
+        f_qk_norm_back = reinterpret_cast<decltype(f_qk_norm_back)>(dlsym(lib, "dare_qk_norm_rope_backward"));
     }
-    if (!f_denoise || !f_denoise_sampled || !f_varlen) {
+    if (!f_denoise || !f_denoise_sampled || !f_varlen || !f_attn_paged || !f_paged_append || !f_qk_norm || !f_qk_norm_back) {
         PyErr_Format(PyExc_RuntimeError, "%s does not export the library's entry points", path);
         return nullptr;
     }
@@ -196,6 +335,10 @@ PyMethodDef methods[] = {
     {"denoise_block", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<denoise_checked<false>>)), METH_FASTCALL, nullptr},
     {"denoise_block_sampled", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<denoise_checked<true>>)), METH_FASTCALL, nullptr},
     {"attn_varlen", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<varlen_checked>)), METH_FASTCALL, nullptr},
+    {"attn_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<attn_paged_checked>)), METH_FASTCALL, nullptr},
+    {"paged_kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<paged_append_checked>)), METH_FASTCALL, nullptr},
+    {"qk_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<qk_norm_checked>)), METH_FASTCALL, nullptr},
+    {"qk_norm_rope_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<qk_norm_back_checked>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -12,6 +12,7 @@ namespace dare {
 
 constexpr uint32_t DEV_LEN_CLAMPED = 1u;
 constexpr uint32_t DEV_WAIT_EXPIRED = 2u;
+constexpr uint32_t DEV_INDEX_OUTSIDE = 4u;
 
 // Upper bound of a single wait, in SM clock cycles (about a second at 2 GHz).
 constexpr long long WAIT_LIMIT_CYCLES = 2000000000LL;
