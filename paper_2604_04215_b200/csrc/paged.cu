@@ -16,6 +16,7 @@
 // Probabilities are rounded to bf16 for the second product (relative 2^-9, averaged over the keys); maximum, sum, products and
 // the joined parts are fp32; the output is rounded once.
 #include <math.h>
+#include <type_traits>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -27,8 +28,8 @@ constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float LN2_F = 0.6931471805599453f;
 
 constexpr int PG_KT = 64;          // keys per tile
+constexpr int PG_LEAST = 3;        // tiles that are a CTA's worth
 constexpr int PG_AHEAD = 2;        // tiles whose pages are looked up before their turn
-constexpr int PG_INFOS = 16;       // descriptors of tiles in flight
 
 struct PagedParams {
     int B, L, Hq, Hkv, g, R, chunks;      // R = L * g packed query rows per (sequence, KV head), in `chunks` of NW * 16
@@ -61,22 +62,29 @@ struct PagedBarriers {
     uint64_t full[STAGES];
     uint64_t empty[STAGES];
     uint64_t merge;
-    TileDesc tile[PG_INFOS];
+    TileDesc tile[STAGES];
+    TileDesc shared_unit[2];           // units that this CTA shares with others: its first one, its last one
+    int pages[PG_AHEAD + 2][32];       // table entries on their way, per lane of the producer
     uint32_t abort_flag;
-    uint32_t arrived;
+    uint32_t arrived[2];
 };
 
+// NW row groups of 16 packed query rows; KS warps share a row group and split every tile's keys between them.  NW = 0: at most 8
+// rows, four key slices (see FewRows).
 template <int D, int NW, int KS>
 struct PagedShape {
+    static constexpr bool FEW = NW == 0;
+    static constexpr int ROWS = FEW ? 8 : NW * 16;
+    static constexpr int WARPS = FEW ? KS : NW * KS;                                  // consumers
     static constexpr int STAGE = 2 * PG_KT * D * 2;
     static constexpr int STAGES = D == 128 ? 3 : 6;
-    // (when the descriptor of tile i + PG_AHEAD is written, tile i - 1 - STAGES has been consumed)
-    static_assert(PG_INFOS >= STAGES + PG_AHEAD + 1, "descriptors");
-    static constexpr int ROUNDS = KS > 1 ? 2 : 1;                                     // of the merge
-    static constexpr int NBK = D / 8 / KS;                                            // column blocks a warp finishes
-    static constexpr int XCH = KS > 1 ? KS * (KS - 1) * NW * NBK / ROUNDS * 512 : 0;  // bytes a round exchanges
-    static constexpr int ML = KS * NW * 16 * 8;
-    static constexpr int SMEM = STAGES * STAGE + XCH + ML + static_cast<int>(sizeof(PagedBarriers<STAGES>)) + 1024;
+    static constexpr int ML = 2 * KS * ROWS * 8;                                      // [unit's parity][KS][ROWS] maximum and sum
+    // Query rows arrive with their unit's first tile, where there is room for them in each of the ring's places; rows are 16 bytes
+    // apart from a power of two (ldmatrix without bank conflicts).
+    static constexpr bool Q_SMEM = ROWS <= 16;
+    static constexpr int Q_ROW = D * 2 + 16;
+    static constexpr int Q_STAGE = Q_SMEM ? ROWS * Q_ROW : 0;
+    static constexpr int SMEM = STAGES * (STAGE + Q_STAGE) + ML + static_cast<int>(sizeof(PagedBarriers<STAGES>)) + 1024;
 };
 
 // The tiles of a sequence of n keys: those of the first positions (window only), then those of the window.
@@ -93,28 +101,661 @@ struct SeqTiles {
     __device__ __forceinline__ int key0(int t) const { return (t < n_sink ? t : win_tile + t - n_sink) * PG_KT; }
 };
 
+// The list of all units' tiles cut into stretches of equal length (to one tile), one per CTA: as many as there are CTAs, but of
+// PG_LEAST tiles at least where that does not leave a unit without a CTA of its own.
+struct Stretches {
+    int n, each, more;        // CTAs that have one; tiles of each; the first `more` have one tile more
+    __device__ __forceinline__ Stretches(int tiles, int units, int ctas) {
+        n = min(max(units, tiles / PG_LEAST), ctas);
+        each = tiles / n;
+        more = tiles - each * n;
+    }
+    __device__ __forceinline__ int begin(int cta) const { return min(cta, n) * each + min(cta, more); }
+    __device__ __forceinline__ int cta_of(int tile) const {
+        const int longer = more * (each + 1);
+        return tile < longer ? tile / (each + 1) : more + (tile - longer) / each;
+    }
+};
+
 __device__ __forceinline__ int seq_keys(const PagedParams& p, int b) {
     return max(0, min(p.kv_lens[b], p.max_pages << p.page_shift));
 }
 
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }      // (a NaN stays one)
+__device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINITY ? -INFINITY : (m + log2f(l)) * LN2_F; }
+
+// Adds a unit's parts up, in the order of the keys (the order of arrival does not show).  A thread has four channels of a row,
+// two rows at once, and asks for JOIN parts at a time: what this costs is trips to L2, one after the other.
+constexpr int JOIN = 8;
+template <int D, int ROWS, int THREADS>
+__device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc& unit) {
+    const TileDesc u = unit;
+    const int items = min(ROWS, p.R - u.chunk * ROWS) * (D / 4);
+    const float2* part_ml = reinterpret_cast<const float2*>(p.part_ml);
+    const float4* part_o = reinterpret_cast<const float4*>(p.part_o);
+    for (int item0 = threadIdx.x; item0 < items; item0 += 2 * THREADS) {
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+        for (int k0 = 0; k0 < u.n_parts; k0 += JOIN) {
+            float2 ml[2][JOIN];
+            float4 x[2][JOIN];
+#pragma unroll
+            for (int k = 0; k < JOIN; ++k) {
+                const int part = min(k0 + k, u.n_parts - 1);           // (beyond the last: the last one, counted 0 times)
+                const int slot = (u.first_cta + part) * 2 + (part == 0 ? u.first_slot : 0);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int item = min(item0 + e * THREADS, items - 1), at = slot * ROWS + item / (D / 4);
+                    ml[e][k] = __ldcg(part_ml + at);
+                    x[e][k] = __ldcg(part_o + static_cast<size_t>(at) * (D / 4) + item % (D / 4));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float mn = m[e];
+#pragma unroll
+                for (int k = 0; k < JOIN; ++k) mn = fmaxf(mn, ml[e][k].x);
+                const float r = mn == -INFINITY ? 0.f : mn, w = fast_exp2(m[e] - r);
+                m[e] = mn;
+                l[e] *= w;
+                acc[e].x *= w; acc[e].y *= w; acc[e].z *= w; acc[e].w *= w;
+#pragma unroll
+                for (int k = 0; k < JOIN; ++k) {
+                    if (k0 + k >= u.n_parts) continue;
+                    const float wk = fast_exp2(ml[e][k].x - r);
+                    l[e] += ml[e][k].y * wk;
+                    acc[e].x += x[e][k].x * wk; acc[e].y += x[e][k].y * wk;
+                    acc[e].z += x[e][k].z * wk; acc[e].w += x[e][k].w * wk;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int item = item0 + e * THREADS;
+            if (item >= items) continue;
+            const float inv = inverse_sum(l[e]);
+            const int rho = u.chunk * ROWS + item / (D / 4), c4 = item % (D / 4), i = rho / p.g, h = u.kvh * p.g + rho - i * p.g;
+            *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(u.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
+                make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
+            if (p.lse != nullptr && c4 == 0)
+                p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(m[e], l[e]);
+        }
+    }
+}
+
+// Shared memory of a CTA.
 template <int D, int NW, int KS>
-__global__ void __launch_bounds__((NW * KS + 1) * 32, 2)
+struct PagedSmem {
+    using S = PagedShape<D, NW, KS>;
+    uint8_t *tiles, *q;                    // [STAGES][STAGE], [STAGES][ROWS][Q_ROW]
+    float2* ml;
+    PagedBarriers<S::STAGES>* bars;
+    __device__ __forceinline__ explicit PagedSmem(uint8_t* raw) {
+        tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+        q = tiles + S::STAGES * S::STAGE;
+        ml = reinterpret_cast<float2*>(q + S::STAGES * S::Q_STAGE);
+        bars = reinterpret_cast<PagedBarriers<S::STAGES>*>(q + S::STAGES * S::Q_STAGE + S::ML);
+    }
+};
+
+// The producer warp: finds this CTA's stretch of the list of tiles (sequence by sequence, in it KV head by KV head, in that chunk
+// by chunk of the query rows) and sends for its tiles.
+template <int D, int NW, int KS>
+__device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorMap* tm_v, const PagedParams& p, const PagedSmem<D, NW, KS>& sm) {
+    using S = PagedShape<D, NW, KS>;
+    constexpr int STAGES = S::STAGES, HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2;
+    PagedBarriers<STAGES>* bars = sm.bars;
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int lane = threadIdx.x & 31;
+    const int HC = p.Hkv * p.chunks;
+    int total = 0, lens = 0;                       // (lens, lane i: keys of sequence (b & ~31) + i)
+    for (int b0 = (p.B - 1) & ~31; b0 >= 0; b0 -= 32) {
+        lens = 0;
+        int nt = 0;
+        if (b0 + lane < p.B) {
+            const int raw = p.kv_lens[b0 + lane];
+            lens = max(0, min(raw, p.max_pages << p.page_shift));
+            if (blockIdx.x == 0 && raw != lens) atomicOr(p.dev_status, DEV_LEN_CLAMPED);
+            nt = SeqTiles(lens, p).n_tiles;
+        }
+        total += __reduce_add_sync(0xffffffffu, nt);
+    }
+    const Stretches st(total * HC, p.B * HC, gridDim.x);
+    const int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
+    if (begin >= end) {
+        if (lane == 0) {
+            bars->tile[0].flags = TILE_NONE;
+            mbar_arrive(&bars->full[0]);
+        }
+        return;
+    }
+    int b = 0, base = 0;                           // the sequence of tile `begin`; its first tile
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+        if (b0 > 0) lens = b0 + lane < p.B ? seq_keys(p, b0 + lane) : 0;
+        const int nt = b0 + lane < p.B ? SeqTiles(lens, p).n_tiles : 0;
+        int incl = nt;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += o;
+        }
+        const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * HC > begin);
+        if (beyond) {
+            const int i = __ffs(beyond) - 1;
+            b = b0 + i;
+            base += __shfl_sync(0xffffffffu, incl - nt, i) * HC;
+            break;
+        }
+        base += __shfl_sync(0xffffffffu, incl, 31) * HC;
+    }
+    // two cursors over the tiles: `ahead` asks for table entries, `now` follows with the copies
+    struct Cursor {
+        int b, u, t, base, lens;
+        SeqTiles sq;
+        __device__ __forceinline__ void next(const PagedParams& p, int HC, int lane) {
+            if (++t < sq.n_tiles) return;
+            t = 0;
+            if (++u < HC) return;
+            u = 0;
+            base += sq.n_tiles * HC;
+            ++b;
+            if ((b & 31) == 0) lens = b + lane < p.B ? seq_keys(p, b + lane) : 0;
+            if (b < p.B) sq = SeqTiles(__shfl_sync(0xffffffffu, lens, b & 31), p);
+        }
+    };
+    const SeqTiles sq0(__shfl_sync(0xffffffffu, lens, b & 31), p);
+    const int u_begin = (begin - base) / sq0.n_tiles;
+    Cursor now = {b, u_begin, begin - base - u_begin * sq0.n_tiles, base, lens, sq0};
+    Cursor ahead = now;
+
+    // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of one half of K or V
+    const int pp_shift = min(p.page_shift, 6), pieces_shift = 6 - pp_shift, rows_pp = 1 << pp_shift;      // (64 keys a tile)
+    const bool active = lane < (NHALF * 2) << pieces_shift;
+    const int piece = lane & ((1 << pieces_shift) - 1), half = (lane >> pieces_shift) % NHALF, is_v = (lane >> pieces_shift) / NHALF;
+    const int pool_rows = (p.n_pages * p.Hkv) << p.page_shift;
+    const uint32_t dst0 = is_v * KV_BYTES + half * HALF + piece * rows_pp * 128;
+    const CUtensorMap* tm = is_v ? tm_v : tm_k;
+    // A lane copies its piece's table entry to shared memory PG_AHEAD tiles before it is needed, so that nothing waits for it.
+    auto visible = [&](const Cursor& c, int key) { return key < c.sq.n && (key < p.sinks || key + rows_pp > c.sq.w0); };
+    auto fetch = [&](int at) {
+        if (at < end) {
+            const int key = ahead.sq.key0(ahead.t) + piece * rows_pp;
+            if (active && visible(ahead, key))
+                cp_async_4(&bars->pages[at % (PG_AHEAD + 2)][lane], p.table + static_cast<long long>(ahead.b) * p.max_pages + (key >> p.page_shift));
+            ahead.next(p, HC, lane);
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int k = 0; k < PG_AHEAD; ++k) fetch(begin + k);
+    int stage = 0, kvh = 0, chunk = 0, c0 = 0, n_parts = 0, slot0 = 0;
+    uint32_t phase = 0;
+    for (int at = begin; at < end; ++at) {
+        fetch(at + PG_AHEAD);
+        const bool first = now.t == 0 || at == begin;
+        if (first) {
+            kvh = p.chunks == 1 ? now.u : now.u / p.chunks;
+            chunk = now.u - kvh * p.chunks;
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag))) break;
+        uint64_t* full = &bars->full[stage];
+        const int key0 = now.sq.key0(now.t), key = key0 + piece * rows_pp;
+        cp_async_wait<PG_AHEAD>();
+        if (active) {
+            int row = pool_rows;                   // behind the pool: zeros
+            if (visible(now, key)) {
+                const int page = bars->pages[at % (PG_AHEAD + 2)][lane];
+                if (page >= 0 && page < p.n_pages) row = ((page * p.Hkv + kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                else atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
+            }
+            // (the bytes may arrive before they are expected: the phase ends with the arrival below)
+            tma_load_2d(sm.tiles + stage * S::STAGE + dst0, tm, full, half * 64, row);
+        }
+        uint32_t bytes = 2 * KV_BYTES;
+        if (first) {
+            if (S::Q_SMEM) {                       // (one chunk: packed query rows 0 .. R - 1 of the sequence)
+                if (lane < p.R) {
+                    const int i = lane / p.g, h = kvh * p.g + lane - i * p.g;
+                    bulk_load(sm.q + stage * S::Q_STAGE + lane * S::Q_ROW, p.q + ((static_cast<size_t>(now.b) * p.L + i) * p.Hq + h) * D, D * 2, full);
+                }
+                bytes += p.R * D * 2;
+            }
+            const int u0 = now.base + now.u * now.sq.n_tiles;
+            c0 = st.cta_of(u0);
+            n_parts = st.cta_of(u0 + now.sq.n_tiles - 1) - c0 + 1;
+            slot0 = st.begin(c0) == u0 ? 0 : 1;
+        }
+        if (lane == 0) {
+            const int n = now.sq.n;
+            TileDesc d;
+            d.flags = (first ? TILE_FIRST : 0) | (now.t == now.sq.n_tiles - 1 || at == end - 1 ? TILE_LAST : 0) | (at == end - 1 ? TILE_END : 0);
+            if (key0 + PG_KT > n || (p.window > 0 && key0 < n - p.window && key0 + PG_KT > p.sinks)) d.flags |= TILE_MASKED;
+            d.b = now.b; d.kvh = kvh; d.chunk = chunk; d.key0 = key0; d.n = n;
+            d.first_cta = c0; d.n_parts = n_parts; d.first_slot = slot0;
+            bars->tile[stage] = d;
+            mbar_arrive_expect_tx(full, bytes);
+        }
+        __syncwarp();
+        now.next(p, HC, lane);
+        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+    }
+}
+
+// What a window hides: key j is hidden from query i (at position n - L + i) if sinks <= j < start + i.
+__device__ __forceinline__ int window_start(const PagedParams& p, int n) { return p.window > 0 ? n - p.L - p.window + 1 : -p.L; }
+
+// V rows that no query may see hold whatever lies there: zeroes those of this warp's keys [koff, koff + KPW) of a tile, so that
+// probability 0 times garbage cannot make a NaN.
+template <int KPW, int NHALF>
+__device__ __forceinline__ void clear_unseen(const PagedParams& p, const TileDesc& ti, uint8_t* vt, int koff) {
+    const int lane = threadIdx.x & 31, start = window_start(p, ti.n);
+    bool wrote = false;
+    for (int o = lane; o < KPW * 8 * NHALF; o += 32) {
+        const int row = koff + (o >> 3) % KPW, half = (o >> 3) / KPW, key = ti.key0 + row;
+        if (key >= ti.n || (key >= p.sinks && key < start)) {
+            *reinterpret_cast<uint4*>(vt + half * PG_KT * 128 + row * 128 + (o & 7) * 16) = make_uint4(0, 0, 0, 0);
+            wrote = true;
+        }
+    }
+    if (wrote) fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// A consumer warp's state for up to 8 query rows: the products are turned round, S^T = K Q^T and O^T = V^T P^T, so that the rows
+// are the MMA's 8 columns and half as many MMAs and registers are needed as with rows for its 16.  Lane (quad, tq): keys (and
+// channels) quad and quad + 8 of each 16, query rows 2 tq and 2 tq + 1.  A warp owns 16 keys of each tile.
+template <int D, int KS>
+struct FewRows {
+    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KPW = PG_KT / KS;
+    static_assert(KPW == 16, "a slice is one MMA's keys");
+    uint32_t qb[D / 16][2];
+    float o[D / 16][4];
+    float m[2], l[2];
+    int row_i[2];              // block positions of this lane's two rows
+
+    __device__ __forceinline__ void place(const PagedParams& p, int) {
+        const int tq = threadIdx.x & 3;
+        row_i[0] = p.L == 1 ? 0 : 2 * tq / p.g;
+        row_i[1] = p.L == 1 ? 0 : (2 * tq + 1) / p.g;
+    }
+    __device__ __forceinline__ void first(const PagedParams&, const TileDesc&, const uint8_t* q_rows, int q_row_bytes, int) {
+        const int lane = threadIdx.x & 31;
+        const uint32_t qa = smem_u32(q_rows) + (lane & 7) * q_row_bytes + (lane >> 3) * 16;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) ldmatrix_x4(qa + j * 64, qb[2 * j][0], qb[2 * j][1], qb[2 * j + 1][0], qb[2 * j + 1][1]);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+    }
+    __device__ __forceinline__ void tile(const PagedParams& p, const TileDesc& ti, uint8_t* kt, int ks) {
+        const int lane = threadIdx.x & 31, quad = lane >> 2, koff = ks * KPW;
+        uint8_t* vt = kt + KV_BYTES;
+        const uint32_t kbase = smem_u32(kt), vbase = smem_u32(vt);
+        const bool masked = ti.flags & TILE_MASKED;
+        if (masked) clear_unseen<KPW, NHALF>(p, ti, vt, koff);
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};          // (two chains of products)
+        {
+            const int key = koff + (lane & 15);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const int ch = 2 * kk + (lane >> 4);
+                uint32_t a[4];
+                ldmatrix_x4(kbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
+                if (kk & 1) mma_bf16_16816(s2, a, qb[kk][0], qb[kk][1]);
+                else mma_bf16_16816(s, a, qb[kk][0], qb[kk][1]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += s2[e];
+        if (masked) {
+            const int start = window_start(p, ti.n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = ti.key0 + koff + quad + (e >> 1) * 8;
+                if (key >= ti.n || (key >= p.sinks && key < start + row_i[e & 1])) s[e] = -INFINITY;
+            }
+        }
+        const float c = p.scale_log2;
+        float mn[2], r[2];
+        bool same = true;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(s[e], s[e + 2]);
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+            mn[e] = fmaxf(m[e], t);
+            r[e] = mn[e] == -INFINITY ? 0.f : mn[e] * c;      // (a row may have seen nothing yet: weights exp2(-inf) = 0)
+            same = same && mn[e] == m[e];
+        }
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = fast_exp2(fmaf(s[e], c, -r[e & 1]));
+        if (__any_sync(0xffffffffu, !same)) {
+            const float f0 = fast_exp2(fmaf(m[0], c, -r[0])), f1 = fast_exp2(fmaf(m[1], c, -r[1]));
+            m[0] = mn[0];
+            m[1] = mn[1];
+            l[0] *= f0;
+            l[1] *= f1;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                o[i][0] *= f0; o[i][1] *= f1;
+                o[i][2] *= f0; o[i][3] *= f1;
+            }
+        }
+        l[0] += w[0] + w[2];
+        l[1] += w[1] + w[3];
+        const uint32_t p0 = movmatrix_trans(pack_bf16(w[0], w[1])), p1 = movmatrix_trans(pack_bf16(w[2], w[3]));
+        const int key = koff + (lane & 7) + (lane >> 4) * 8;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const int ch = 2 * i + ((lane >> 3) & 1);
+            uint32_t a[4];
+            ldmatrix_x4_trans(vbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
+            mma_bf16_16816(o[i], a, p0, p1);
+        }
+    }
+    // The unit's end in this CTA: every warp lays its part down over its own keys of the tile that it has just read, then the rows are
+    // added up four channels at a time.  `kt` is the tile's place, ml [KS][8].
+    template <typename Sync>
+    __device__ __forceinline__ bool finish(const PagedParams& p, const TileDesc& ti, uint8_t* kt, float2* ml, int ks, int slot, Sync&& sync) {
+        // place of row q of slice s: pieces of 16 keys of one half of K or V are 2 KB; 8 / (2 NHALF) rows in each
+        constexpr int PER = 8 / (2 * NHALF);
+        auto at = [&](int s, int q) {
+            return reinterpret_cast<float*>(kt + (q / PER) * HALF + s * KPW * 128 + (q % PER) * (D * 4 + 16) + (q / PER) * (PER * 16));
+        };
+        const int lane = threadIdx.x & 31, quad = lane >> 2, tq = lane & 3;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 4);
+            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 8);
+            l[e] += __shfl_xor_sync(0xffffffffu, l[e], 16);
+            if (quad == 0) ml[ks * 8 + 2 * tq + e] = make_float2(m[e] * p.scale_log2, l[e]);
+            float* x = at(ks, 2 * tq + e);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                x[i * 16 + quad] = o[i][e];
+                x[i * 16 + quad + 8] = o[i][e + 2];
+            }
+        }
+        if (!sync()) return false;
+        const bool whole = ti.n_parts == 1;
+        for (int item = threadIdx.x; item < p.R * (D / 4); item += KS * 32) {
+            const int q = item / (D / 4), c4 = item % (D / 4);
+            float2 part[KS];
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                part[s] = ml[s * 8 + q];
+                top = fmaxf(top, part[s].x);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const float w = fast_exp2(part[s].x - ref);
+                const float4 x = *reinterpret_cast<const float4*>(at(s, q) + c4 * 4);
+                sum += part[s].y * w;
+                acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
+            }
+            if (whole) {
+                const float inv = inverse_sum(sum);
+                const int i = p.L == 1 ? 0 : q / p.g, h = ti.kvh * p.g + q - i * p.g;
+                *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(ti.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
+                    make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                if (p.lse != nullptr && c4 == 0) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h) * p.L + i] = log_sum(top, sum);
+            } else {
+                *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * 8 + q) * D + c4 * 4) = acc;
+                if (c4 == 0) reinterpret_cast<float2*>(p.part_ml)[slot * 8 + q] = make_float2(top, sum);
+            }
+        }
+        return true;
+    }
+};
+
+// A consumer warp's state for 16 query rows (the MMA's rows) and 64 / KS of each tile's keys.  Lane (quad, tq): rows quad and
+// quad + 8, keys (and channels) 2 tq and 2 tq + 1 of each 8.
+template <int D, int NW, int KS>
+struct ManyRows {
+    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KPW = PG_KT / KS, ROWS = NW * 16;
+    static constexpr int NBK = D / 8 / KS;       // blocks of 8 columns that a warp finishes
+    static constexpr bool Q_SMEM = PagedShape<D, NW, KS>::Q_SMEM;
+    static_assert(KS * (KS - 1) * NW * NBK * 512 <= PagedShape<D, NW, KS>::STAGE, "the merge goes through the last tile's place in the ring");
+    uint32_t qf[D / 16][4];
+    float oacc[D / 8][4];
+    float m0, m1, l0, l1;
+    int i0, i1, g0, g1;                          // block positions of this lane's two rows, and heads within the group
+    bool live0, live1;
+
+    __device__ __forceinline__ void place(const PagedParams& p, int warp, int chunk = 0) {
+        const int rho0 = chunk * ROWS + warp % NW * 16 + ((threadIdx.x & 31) >> 2), rho1 = rho0 + 8;
+        live0 = rho0 < p.R;
+        live1 = rho1 < p.R;
+        i0 = live0 ? rho0 / p.g : 0;
+        i1 = live1 ? rho1 / p.g : 0;
+        g0 = live0 ? rho0 - i0 * p.g : 0;
+        g1 = live1 ? rho1 - i1 * p.g : 0;
+    }
+    __device__ __forceinline__ void first(const PagedParams& p, const TileDesc& ti, const uint8_t* q_rows, int q_row_bytes, int warp) {
+        const int lane = threadIdx.x & 31, tq = lane & 3;
+        if (Q_SMEM) {
+            const uint32_t qa = smem_u32(q_rows) + (lane & 15) * q_row_bytes + (lane >> 4) * 16;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) ldmatrix_x4(qa + kk * 32, qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3]);
+        } else {
+            place(p, warp, ti.chunk);
+            const uint32_t* q0 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + ti.kvh * p.g + g0) * D);
+            const uint32_t* q1 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + ti.kvh * p.g + g1) * D);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                qf[kk][0] = live0 ? q0[kk * 8 + tq] : 0u;
+                qf[kk][1] = live1 ? q1[kk * 8 + tq] : 0u;
+                qf[kk][2] = live0 ? q0[kk * 8 + 4 + tq] : 0u;
+                qf[kk][3] = live1 ? q1[kk * 8 + 4 + tq] : 0u;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) oacc[n][0] = oacc[n][1] = oacc[n][2] = oacc[n][3] = 0.f;
+        m0 = m1 = -INFINITY;
+        l0 = l1 = 0.f;
+    }
+    __device__ __forceinline__ void tile(const PagedParams& p, const TileDesc& ti, uint8_t* kt, int warp) {
+        const int lane = threadIdx.x & 31, tq = lane & 3, mi = lane >> 3, rin = lane & 7, koff = warp / NW * KPW;
+        uint8_t* vt = kt + KV_BYTES;
+        const uint32_t kbase = smem_u32(kt), vbase = smem_u32(vt);
+        const float c = p.scale_log2;
+        const bool masked = ti.flags & TILE_MASKED;
+        if (masked) clear_unseen<KPW, NHALF>(p, ti, vt, koff);
+        // S = Q K^T for this warp's keys
+        float sacc[KPW / 8][4];
+#pragma unroll
+        for (int nb = 0; nb < KPW / 8; ++nb) sacc[nb][0] = sacc[nb][1] = sacc[nb][2] = sacc[nb][3] = 0.f;
+#pragma unroll
+        for (int kq = 0; kq < D / 32; ++kq) {
+            uint32_t kf[KPW / 8][4];
+#pragma unroll
+            for (int nb = 0; nb < KPW / 8; ++nb) {
+                const int key = koff + nb * 8 + rin, ch = 4 * kq + mi;
+                ldmatrix_x4(kbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), kf[nb][0], kf[nb][1], kf[nb][2], kf[nb][3]);
+            }
+#pragma unroll
+            for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq], kf[nb][0], kf[nb][1]);
+#pragma unroll
+            for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq + 1], kf[nb][2], kf[nb][3]);
+        }
+        if (masked) {
+            const int start = window_start(p, ti.n);
+#pragma unroll
+            for (int nb = 0; nb < KPW / 8; ++nb) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = ti.key0 + koff + nb * 8 + tq * 2 + (e & 1);
+                    if (key >= ti.n || (key >= p.sinks && key < start + (e < 2 ? i0 : i1))) sacc[nb][e] = -INFINITY;
+                }
+            }
+        }
+        float tmax0 = -INFINITY, tmax1 = -INFINITY;
+#pragma unroll
+        for (int nb = 0; nb < KPW / 8; ++nb) {
+            tmax0 = fmaxf(tmax0, fmaxf(sacc[nb][0], sacc[nb][1]));
+            tmax1 = fmaxf(tmax1, fmaxf(sacc[nb][2], sacc[nb][3]));
+        }
+        tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 1));
+        tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 2));
+        tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 1));
+        tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 2));
+        // (a row may have seen nothing yet: its reference is then 0, its weights exp2(-inf) = 0)
+        const float mn0 = fmaxf(m0, tmax0), mn1 = fmaxf(m1, tmax1);
+        const float r0 = mn0 == -INFINITY ? 0.f : mn0 * c, r1 = mn1 == -INFINITY ? 0.f : mn1 * c;
+        const bool moved = __any_sync(0xffffffffu, mn0 != m0 || mn1 != m1);
+        float ps0 = 0.f, ps1 = 0.f;
+        uint32_t pa[KPW / 16][4];
+#pragma unroll
+        for (int nb = 0; nb < KPW / 8; ++nb) {
+            const float e0 = fast_exp2(fmaf(sacc[nb][0], c, -r0)), e1 = fast_exp2(fmaf(sacc[nb][1], c, -r0));
+            const float e2 = fast_exp2(fmaf(sacc[nb][2], c, -r1)), e3 = fast_exp2(fmaf(sacc[nb][3], c, -r1));
+            ps0 += e0 + e1;
+            ps1 += e2 + e3;
+            pa[nb >> 1][(nb & 1) * 2 + 0] = pack_bf16(e0, e1);
+            pa[nb >> 1][(nb & 1) * 2 + 1] = pack_bf16(e2, e3);
+        }
+        if (moved) {
+            const float a0 = fast_exp2(fmaf(m0, c, -r0)), a1 = fast_exp2(fmaf(m1, c, -r1));
+            m0 = mn0;
+            m1 = mn1;
+            l0 *= a0;
+            l1 *= a1;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+                oacc[n][0] *= a0; oacc[n][1] *= a0;
+                oacc[n][2] *= a1; oacc[n][3] *= a1;
+            }
+        }
+        l0 += ps0;
+        l1 += ps1;
+        // O += P V
+#pragma unroll
+        for (int kk = 0; kk < KPW / 16; ++kk) {
+            const int key = koff + kk * 16 + (mi & 1) * 8 + rin;
+#pragma unroll
+            for (int nbp = 0; nbp < D / 16; ++nbp) {
+                const int ch = 2 * nbp + (mi >> 1);
+                uint32_t v0, v1, v2, v3;
+                ldmatrix_x4_trans(vbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), v0, v1, v2, v3);
+                mma_bf16_16816(oacc[2 * nbp], pa[kk], v0, v1);
+                mma_bf16_16816(oacc[2 * nbp + 1], pa[kk], v2, v3);
+            }
+        }
+    }
+    // The unit's end in this CTA: merge the key slices through this tile's place in the ring; each slice's warp finishes its share of
+    // the columns.  ml [KS][ROWS].
+    template <typename Sync>
+    __device__ __forceinline__ bool finish(const PagedParams& p, const TileDesc& ti, uint8_t* kt, float2* ml, int warp, int slot, Sync&& sync) {
+        const int lane = threadIdx.x & 31, quad = lane >> 2, tq = lane & 3, rg = warp % NW, ks = warp / NW;
+        l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+        l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+        float tm0 = m0 * p.scale_log2, tm1 = m1 * p.scale_log2;          // log2 domain
+        if (KS > 1) {
+            if (tq == 0) {
+                ml[ks * ROWS + rg * 16 + quad] = make_float2(tm0, l0);
+                ml[ks * ROWS + rg * 16 + quad + 8] = make_float2(tm1, l1);
+            }
+            if (!sync()) return false;
+            float w0[KS], w1[KS];
+            float2 ml0[KS], ml1[KS];
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                ml0[o] = ml[o * ROWS + rg * 16 + quad];
+                ml1[o] = ml[o * ROWS + rg * 16 + quad + 8];
+                tm0 = fmaxf(tm0, ml0[o].x);
+                tm1 = fmaxf(tm1, ml1[o].x);
+            }
+            l0 = l1 = 0.f;
+            const float r0 = tm0 == -INFINITY ? 0.f : tm0, r1 = tm1 == -INFINITY ? 0.f : tm1;
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                w0[o] = fast_exp2(ml0[o].x - r0);
+                w1[o] = fast_exp2(ml1[o].x - r1);
+                l0 += ml0[o].y * w0[o];
+                l1 += ml1[o].y * w1[o];
+            }
+            float4* xch = reinterpret_cast<float4*>(kt);       // [finishing slice][other slices][row group][block of 8 columns][lane]
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                if (o == ks) continue;
+#pragma unroll
+                for (int i = 0; i < NBK; ++i) {
+                    const float (&v)[4] = oacc[o * NBK + i];
+                    xch[(((o * (KS - 1) + (ks < o ? ks : ks - 1)) * NW + rg) * NBK + i) * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+            if (!sync()) return false;
+#pragma unroll
+            for (int o = 0; o < KS; ++o) {
+                if (o != ks) continue;
+#pragma unroll
+                for (int i = 0; i < NBK; ++i) {
+                    float (&v)[4] = oacc[o * NBK + i];
+                    v[0] *= w0[o]; v[1] *= w0[o]; v[2] *= w1[o]; v[3] *= w1[o];
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        if (s == o) continue;
+                        const float4 x = xch[(((o * (KS - 1) + (s < o ? s : s - 1)) * NW + rg) * NBK + i) * 32 + lane];
+                        v[0] += x.x * w0[s]; v[1] += x.y * w0[s];
+                        v[2] += x.z * w1[s]; v[3] += x.w * w1[s];
+                    }
+                }
+            }
+        }
+        const bool whole = ti.n_parts == 1;
+        const float inv0 = whole ? inverse_sum(l0) : 1.f, inv1 = whole ? inverse_sum(l1) : 1.f;
+        const int h0 = ti.kvh * p.g + g0, h1 = ti.kvh * p.g + g1;
+        const size_t orow0 = (static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + h0, orow1 = (static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + h1;
+        float* po = p.part_o + static_cast<size_t>(slot) * ROWS * D;
+#pragma unroll
+        for (int o = 0; o < KS; ++o) {
+            if (o != ks) continue;
+#pragma unroll
+            for (int i = 0; i < NBK; ++i) {
+                const float (&v)[4] = oacc[o * NBK + i];
+                const int col = (o * NBK + i) * 8 + tq * 2;
+                if (whole) {
+                    if (live0) *reinterpret_cast<uint32_t*>(p.out + orow0 * D + col) = pack_bf16(v[0] * inv0, v[1] * inv0);
+                    if (live1) *reinterpret_cast<uint32_t*>(p.out + orow1 * D + col) = pack_bf16(v[2] * inv1, v[3] * inv1);
+                } else {
+                    if (live0) *reinterpret_cast<float2*>(po + (rg * 16 + quad) * D + col) = make_float2(v[0], v[1]);
+                    if (live1) *reinterpret_cast<float2*>(po + (rg * 16 + quad + 8) * D + col) = make_float2(v[2], v[3]);
+                }
+            }
+        }
+        if (ks == 0 && tq == 0) {
+            if (whole) {
+                if (p.lse != nullptr) {
+                    if (live0) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h0) * p.L + i0] = log_sum(tm0, l0);
+                    if (live1) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h1) * p.L + i1] = log_sum(tm1, l1);
+                }
+            } else {
+                float2* pm = reinterpret_cast<float2*>(p.part_ml) + static_cast<size_t>(slot) * ROWS + rg * 16 + quad;
+                pm[0] = make_float2(tm0, l0);
+                pm[8] = make_float2(tm1, l1);
+            }
+        }
+        return true;
+    }
+};
+
+template <int D, int NW, int KS>
+__global__ void __launch_bounds__((PagedShape<D, NW, KS>::WARPS + 1) * 32, 2)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
     using S = PagedShape<D, NW, KS>;
-    constexpr int STAGES = S::STAGES, STAGE = S::STAGE, NBK = S::NBK;
-    constexpr int HALF = PG_KT * 128;            // one 64-column half of a tile: 64 rows x 128 bytes
-    constexpr int NHALF = D / 64;
-    constexpr int KV_BYTES = PG_KT * D * 2;
-    constexpr int NCW = NW * KS, ROWS = NW * 16;
-    constexpr int KPW = PG_KT / KS;              // keys per warp per tile
-
+    constexpr int STAGES = S::STAGES, NCW = S::WARPS;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float4* xch = reinterpret_cast<float4*>(tiles + STAGES * STAGE);
-    float2* xch_ml = reinterpret_cast<float2*>(tiles + STAGES * STAGE + S::XCH);          // [KS][NW * 16]
-    PagedBarriers<STAGES>* bars = reinterpret_cast<PagedBarriers<STAGES>*>(tiles + STAGES * STAGE + S::XCH + S::ML);
+    const PagedSmem<D, NW, KS> sm(smem_raw);
+    PagedBarriers<STAGES>* bars = sm.bars;
     volatile uint32_t* abort_flag = &bars->abort_flag;
-
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     if (threadIdx.x == NCW * 32) {
@@ -128,138 +769,19 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         prefetch_tensormap(&tm_k);
         prefetch_tensormap(&tm_v);
     }
+    if (S::Q_SMEM) {                             // rows that are no query's: zero, once
+        for (int o = threadIdx.x; o < STAGES * S::Q_STAGE / 16; o += (NCW + 1) * 32) reinterpret_cast<uint4*>(sm.q)[o] = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
     __syncthreads();
     pdl_wait();
 
     if (warp == NCW) {
-        // ---------------- producer.  This CTA's stretch of the list of tiles: sequence by sequence, in it KV head by KV head
-        // (and chunk by chunk of its query rows).
-        const int HC = p.Hkv * p.chunks;
-        long long total = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const int b = b0 + lane;
-            int nt = 0;
-            if (b < p.B) {
-                const int raw = p.kv_lens[b];
-                if (blockIdx.x == 0 && (raw < 0 || raw > (p.max_pages << p.page_shift))) atomicOr(p.dev_status, DEV_LEN_CLAMPED);
-                nt = SeqTiles(seq_keys(p, b), p).n_tiles;
-            }
-            total += __reduce_add_sync(0xffffffffu, nt);      // (32 x 2^24 tiles fit 32 bits)
-        }
-        total *= HC;
-        const long long ctas = total < gridDim.x ? total : gridDim.x;
-        const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
-        const long long end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
-        if (begin >= end) {
-            if (lane == 0) {
-                bars->tile[0].flags = TILE_NONE;
-                mbar_arrive(&bars->full[0]);
-            }
-        } else {
-            // the sequence of tile `begin`
-            int b = 0, lens = 0;                   // (lane i: keys of sequence (b & ~31) + i)
-            long long base = 0;                    // first tile of sequence b
-            for (int b0 = 0; b0 < p.B; b0 += 32) {
-                lens = b0 + lane < p.B ? seq_keys(p, b0 + lane) : 0;
-                const int nt = b0 + lane < p.B ? SeqTiles(lens, p).n_tiles : 0;
-                int incl = nt;
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const int o = __shfl_up_sync(0xffffffffu, incl, off);
-                    if (lane >= off) incl += o;
-                }
-                const long long after = base + static_cast<long long>(incl) * HC;
-                const unsigned beyond = __ballot_sync(0xffffffffu, after > begin);
-                if (beyond) {
-                    const int i = __ffs(beyond) - 1;
-                    b = b0 + i;
-                    base += static_cast<long long>(__shfl_sync(0xffffffffu, incl - nt, i)) * HC;
-                    break;
-                }
-                base += static_cast<long long>(__shfl_sync(0xffffffffu, incl, 31)) * HC;
-            }
-            // a cursor over the tiles, PG_AHEAD in front of the copies
-            SeqTiles sq(__shfl_sync(0xffffffffu, lens, b & 31), p);
-            int u = static_cast<int>((begin - base) / sq.n_tiles), t = static_cast<int>((begin - base) % sq.n_tiles);
-            long long at = begin;
-
-            // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of one half of K or V
-            const int pieces = PG_KT >> min(p.page_shift, 6), rows_pp = PG_KT / pieces;
-            const bool active = lane < pieces * NHALF * 2;
-            const int piece = lane % pieces, half = lane / pieces % NHALF, is_v = lane / pieces / NHALF;
-            const int pool_rows = (p.n_pages * p.Hkv) << p.page_shift;
-            const uint32_t dst0 = is_v * KV_BYTES + half * HALF + piece * rows_pp * 128;
-            int rows_q[PG_AHEAD + 1];              // pool rows of this lane's pieces of the next tiles
-            int kvh = 0, c0 = 0, n_parts = 0, slot0 = 0;
-            auto look_up = [&]() -> int {          // the cursor's tile: its descriptor, this lane's pool row; then the next one
-                if (at >= end) return 0;
-                if (t == 0 || at == begin) {       // tile x lies in the CTA ceil((x + 1) ctas / total) - 1
-                    const long long u0 = base + static_cast<long long>(u) * sq.n_tiles, u1 = u0 + sq.n_tiles;
-                    c0 = static_cast<int>(((u0 + 1) * ctas + total - 1) / total) - 1;
-                    n_parts = static_cast<int>((u1 * ctas + total - 1) / total) - c0;
-                    slot0 = total * c0 / ctas >= u0 ? 0 : 1;
-                    kvh = u / p.chunks;
-                }
-                const int key0 = sq.key0(t);
-                if (lane == 0) {
-                    TileDesc d;
-                    d.flags = (t == 0 || at == begin ? TILE_FIRST : 0) | (t == sq.n_tiles - 1 || at == end - 1 ? TILE_LAST : 0) |
-                              (at == end - 1 ? TILE_END : 0);
-                    if (key0 + PG_KT > sq.n || (p.window > 0 && key0 < sq.n - p.window && key0 + PG_KT > p.sinks)) d.flags |= TILE_MASKED;
-                    d.b = b; d.kvh = kvh; d.chunk = u % p.chunks; d.key0 = key0; d.n = sq.n;
-                    d.first_cta = c0; d.n_parts = n_parts; d.first_slot = slot0;
-                    bars->tile[(at - begin) % PG_INFOS] = d;
-                }
-                int row = pool_rows;               // behind the pool: zeros
-                const int key = key0 + piece * rows_pp;
-                if (active && key < sq.n && (key < p.sinks || key + rows_pp > sq.w0)) {
-                    const int page = p.table[static_cast<long long>(b) * p.max_pages + (key >> p.page_shift)];
-                    if (page >= 0 && page < p.n_pages) row = ((page * p.Hkv + kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
-                    else atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
-                }
-                ++at;
-                if (++t == sq.n_tiles) {
-                    t = 0;
-                    if (++u == HC) {
-                        u = 0;
-                        base += static_cast<long long>(sq.n_tiles) * HC;
-                        ++b;
-                        if ((b & 31) == 0) lens = b + lane < p.B ? seq_keys(p, b + lane) : 0;
-                        if (b < p.B) sq = SeqTiles(__shfl_sync(0xffffffffu, lens, b & 31), p);
-                    }
-                }
-                return row;
-            };
-#pragma unroll
-            for (int i = 0; i < PG_AHEAD; ++i) rows_q[i] = look_up();
-            int stage = 0;
-            uint32_t phase = 0;
-            for (long long i = begin; i < end; ++i) {
-                rows_q[PG_AHEAD] = look_up();
-                if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag))) break;
-                if (lane == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * KV_BYTES);
-                __syncwarp();
-                if (active) tma_load_2d(tiles + stage * STAGE + dst0, is_v ? &tm_v : &tm_k, &bars->full[stage], half * 64, rows_q[0]);
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < PG_AHEAD; ++k) rows_q[k] = rows_q[k + 1];
-                if (++stage == STAGES) { stage = 0; phase ^= 1; }
-            }
-        }
+        produce<D, NW, KS>(&tm_k, &tm_v, p, sm);
     } else {
-        // ---------------- consumers
-        const int rg = warp % NW, ks = warp / NW;          // row group, key slice
-        const int quad = lane >> 2, tq = lane & 3;
-        const int mi = lane >> 3, rin = lane & 7;
-        const int koff = ks * KPW;
-        const float c = p.scale_log2;
-        int stage = 0;
-        uint32_t phase = 0, merge_phase = 0, n_tile = 0;
-        uint32_t qf[D / 16][4];
-        float oacc[D / 8][4];
-        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-        int i0 = 0, i1 = 0, h0 = 0, h1 = 0;                // block positions and heads of this lane's two rows
-        bool live0 = false, live1 = false;
+        std::conditional_t<S::FEW, FewRows<D, KS>, ManyRows<D, S::FEW ? 1 : NW, KS>> c;
+        int stage = 0, n_shared = 0;
+        uint32_t phase = 0, merge_phase = 0, parity = 0;
         // a barrier among the consumer warps, bounded as all waits are
         auto merge_sync = [&]() -> bool {
             __syncwarp();
@@ -268,277 +790,47 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             merge_phase ^= 1;
             return __all_sync(0xffffffffu, ok);
         };
+        c.place(p, warp);
         while (true) {
             if (!__all_sync(0xffffffffu, mbar_wait(&bars->full[stage], phase, abort_flag))) break;
-            const TileDesc ti = bars->tile[n_tile % PG_INFOS];
-            ++n_tile;
+            const TileDesc ti = bars->tile[stage];
             if (ti.flags & TILE_NONE) break;
-            uint8_t* kt = tiles + stage * STAGE;
-            uint8_t* vt = kt + KV_BYTES;
-            const uint32_t kbase = smem_u32(kt), vbase = smem_u32(vt);
-            if (ti.flags & TILE_FIRST) {
-                const int rho0 = ti.chunk * ROWS + rg * 16 + quad, rho1 = rho0 + 8;
-                live0 = rho0 < p.R;
-                live1 = rho1 < p.R;
-                i0 = live0 ? rho0 / p.g : 0;
-                i1 = live1 ? rho1 / p.g : 0;
-                h0 = ti.kvh * p.g + (live0 ? rho0 % p.g : 0);
-                h1 = ti.kvh * p.g + (live1 ? rho1 % p.g : 0);
-                const uint32_t* q0 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + h0) * D);
-                const uint32_t* q1 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + h1) * D);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    qf[kk][0] = live0 ? q0[kk * 8 + tq] : 0u;
-                    qf[kk][1] = live1 ? q1[kk * 8 + tq] : 0u;
-                    qf[kk][2] = live0 ? q0[kk * 8 + 4 + tq] : 0u;
-                    qf[kk][3] = live1 ? q1[kk * 8 + 4 + tq] : 0u;
-                }
-#pragma unroll
-                for (int n = 0; n < D / 8; ++n) oacc[n][0] = oacc[n][1] = oacc[n][2] = oacc[n][3] = 0.f;
-                m0 = m1 = -INFINITY;
-                l0 = l1 = 0.f;
-            }
-            const bool masked = ti.flags & TILE_MASKED;
-            if (masked) {
-                // V rows that no query may see hold whatever lies there: zero this warp's, so that probability 0 times
-                // garbage cannot make a NaN
-                const int w0 = p.window > 0 ? ti.n - p.L - p.window + 1 : 0;
-                bool wrote = false;
-                for (int o = lane; o < KPW * 8 * NHALF; o += 32) {
-                    const int row = koff + (o >> 3) % KPW, half = (o >> 3) / KPW, key = ti.key0 + row;
-                    if (key >= ti.n || (key >= p.sinks && key < w0)) {
-                        *reinterpret_cast<uint4*>(vt + half * HALF + row * 128 + (o & 7) * 16) = make_uint4(0, 0, 0, 0);
-                        wrote = true;
-                    }
-                }
-                if (wrote) fence_proxy_async_smem();
-                __syncwarp();
-            }
-            // S = Q K^T for this warp's keys
-            float sacc[KPW / 8][4];
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) sacc[nb][0] = sacc[nb][1] = sacc[nb][2] = sacc[nb][3] = 0.f;
-#pragma unroll
-            for (int kq = 0; kq < D / 32; ++kq) {
-                uint32_t kf[KPW / 8][4];
-#pragma unroll
-                for (int nb = 0; nb < KPW / 8; ++nb) {
-                    const int key = koff + nb * 8 + rin, ch = 4 * kq + mi;
-                    ldmatrix_x4(kbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), kf[nb][0], kf[nb][1], kf[nb][2], kf[nb][3]);
-                }
-#pragma unroll
-                for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq], kf[nb][0], kf[nb][1]);
-#pragma unroll
-                for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq + 1], kf[nb][2], kf[nb][3]);
-            }
-            if (masked) {
-                // keys [sinks, start of the row's window) and from n on do not count
-                const int no_window = p.window > 0 ? 0 : ti.n + p.L;
-                const int s0 = ti.n - p.L + i0 - p.window + 1 - no_window, s1 = ti.n - p.L + i1 - p.window + 1 - no_window;
-#pragma unroll
-                for (int nb = 0; nb < KPW / 8; ++nb) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = ti.key0 + koff + nb * 8 + tq * 2 + (e & 1);
-                        if (key >= ti.n || (key >= p.sinks && key < (e < 2 ? s0 : s1))) sacc[nb][e] = -INFINITY;
-                    }
-                }
-            }
-            float tmax0 = -INFINITY, tmax1 = -INFINITY;
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) {
-                tmax0 = fmaxf(tmax0, fmaxf(sacc[nb][0], sacc[nb][1]));
-                tmax1 = fmaxf(tmax1, fmaxf(sacc[nb][2], sacc[nb][3]));
-            }
-            tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 1));
-            tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 2));
-            tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 1));
-            tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 2));
-            // (a row may have seen nothing yet: its reference is then 0, its weights exp2(-inf) = 0)
-            const float mn0 = fmaxf(m0, tmax0), mn1 = fmaxf(m1, tmax1);
-            const float r0 = mn0 == -INFINITY ? 0.f : mn0 * c, r1 = mn1 == -INFINITY ? 0.f : mn1 * c;
-            const bool moved = __any_sync(0xffffffffu, mn0 != m0 || mn1 != m1);
-            float ps0 = 0.f, ps1 = 0.f;
-            uint32_t pa[KPW / 16][4];
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) {
-                const float e0 = fast_exp2(fmaf(sacc[nb][0], c, -r0)), e1 = fast_exp2(fmaf(sacc[nb][1], c, -r0));
-                const float e2 = fast_exp2(fmaf(sacc[nb][2], c, -r1)), e3 = fast_exp2(fmaf(sacc[nb][3], c, -r1));
-                ps0 += e0 + e1;
-                ps1 += e2 + e3;
-                pa[nb >> 1][(nb & 1) * 2 + 0] = pack_bf16(e0, e1);
-                pa[nb >> 1][(nb & 1) * 2 + 1] = pack_bf16(e2, e3);
-            }
-            if (moved) {
-                const float a0 = fast_exp2(fmaf(m0, c, -r0)), a1 = fast_exp2(fmaf(m1, c, -r1));
-                m0 = mn0;
-                m1 = mn1;
-                l0 *= a0;
-                l1 *= a1;
-#pragma unroll
-                for (int n = 0; n < D / 8; ++n) {
-                    oacc[n][0] *= a0; oacc[n][1] *= a0;
-                    oacc[n][2] *= a1; oacc[n][3] *= a1;
-                }
-            }
-            l0 += ps0;
-            l1 += ps1;
-            // O += P V
-#pragma unroll
-            for (int kk = 0; kk < KPW / 16; ++kk) {
-                const int key = koff + kk * 16 + (mi & 1) * 8 + rin;
-#pragma unroll
-                for (int nbp = 0; nbp < D / 16; ++nbp) {
-                    const int ch = 2 * nbp + (mi >> 1);
-                    uint32_t v0, v1, v2, v3;
-                    ldmatrix_x4_trans(vbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), v0, v1, v2, v3);
-                    mma_bf16_16816(oacc[2 * nbp], pa[kk], v0, v1);
-                    mma_bf16_16816(oacc[2 * nbp + 1], pa[kk], v2, v3);
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->empty[stage]);
+            uint8_t* kt = sm.tiles + stage * S::STAGE;
+            if (ti.flags & TILE_FIRST) c.first(p, ti, sm.q + stage * S::Q_STAGE, S::Q_ROW, warp);
+            c.tile(p, ti, kt, warp);
+            const int this_stage = stage;
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
-            if (!(ti.flags & TILE_LAST)) continue;
-
-            // ---------------- the unit's end in this CTA: merge the key slices; each slice's warp finishes its share of the columns
-            float tl0 = l0 + __shfl_xor_sync(0xffffffffu, l0, 1), tl1 = l1 + __shfl_xor_sync(0xffffffffu, l1, 1);
-            tl0 += __shfl_xor_sync(0xffffffffu, tl0, 2);
-            tl1 += __shfl_xor_sync(0xffffffffu, tl1, 2);
-            float tm0 = m0 * c, tm1 = m1 * c;              // log2 domain
-            float w0[KS], w1[KS];
-            if (KS > 1) {
-                if (tq == 0) {
-                    xch_ml[ks * ROWS + rg * 16 + quad] = make_float2(tm0, tl0);
-                    xch_ml[ks * ROWS + rg * 16 + quad + 8] = make_float2(tm1, tl1);
-                }
-                if (!merge_sync()) break;
-                float2 ml0[KS], ml1[KS];
-#pragma unroll
-                for (int o = 0; o < KS; ++o) {
-                    ml0[o] = xch_ml[o * ROWS + rg * 16 + quad];
-                    ml1[o] = xch_ml[o * ROWS + rg * 16 + quad + 8];
-                    tm0 = fmaxf(tm0, ml0[o].x);
-                    tm1 = fmaxf(tm1, ml1[o].x);
-                }
-                tl0 = tl1 = 0.f;
-#pragma unroll
-                for (int o = 0; o < KS; ++o) {
-                    w0[o] = tm0 == -INFINITY ? 0.f : fast_exp2(ml0[o].x - tm0);
-                    w1[o] = tm1 == -INFINITY ? 0.f : fast_exp2(ml1[o].x - tm1);
-                    tl0 += ml0[o].y * w0[o];
-                    tl1 += ml1[o].y * w1[o];
-                }
-                constexpr int NBR = NBK / S::ROUNDS;       // column blocks of a round
-                bool ok = true;
-#pragma unroll
-                for (int r = 0; r < S::ROUNDS; ++r) {
-#pragma unroll
-                    for (int o = 0; o < KS; ++o) {
-                        if (o == ks) continue;
-#pragma unroll
-                        for (int i = 0; i < NBR; ++i) {
-                            const float (&v)[4] = oacc[o * NBK + r * NBR + i];
-                            xch[(((o * (KS - 1) + (ks < o ? ks : ks - 1)) * NW + rg) * NBR + i) * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
-                        }
-                    }
-                    ok = merge_sync();
-                    if (!ok) break;
-#pragma unroll
-                    for (int o = 0; o < KS; ++o) {
-                        if (o != ks) continue;
-#pragma unroll
-                        for (int i = 0; i < NBR; ++i) {
-                            float (&v)[4] = oacc[o * NBK + r * NBR + i];
-                            v[0] *= w0[o]; v[1] *= w0[o]; v[2] *= w1[o]; v[3] *= w1[o];
-#pragma unroll
-                            for (int s = 0; s < KS; ++s) {
-                                if (s == o) continue;
-                                const float4 x = xch[(((o * (KS - 1) + (s < o ? s : s - 1)) * NW + rg) * NBR + i) * 32 + lane];
-                                v[0] += x.x * w0[s]; v[1] += x.y * w0[s];
-                                v[2] += x.z * w1[s]; v[3] += x.w * w1[s];
-                            }
-                        }
-                    }
-                    ok = merge_sync();
-                    if (!ok) break;
-                }
-                if (!ok) break;
+            if (!(ti.flags & TILE_LAST)) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->empty[this_stage]);
+                continue;
             }
-            const bool whole = ti.n_parts == 1;
-            const float inv0 = whole ? (tl0 > 0.f ? 1.f / tl0 : tl0 == 0.f ? 0.f : tl0) : 1.f;      // (a NaN sum stays one)
-            const float inv1 = whole ? (tl1 > 0.f ? 1.f / tl1 : tl1 == 0.f ? 0.f : tl1) : 1.f;
-            const size_t orow0 = (static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + h0, orow1 = (static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + h1;
             const int slot = blockIdx.x * 2 + (static_cast<int>(blockIdx.x) == ti.first_cta ? ti.first_slot : 0);
-            float* po = p.part_o + static_cast<size_t>(slot) * ROWS * D;
-#pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                if (o != ks) continue;
-#pragma unroll
-                for (int i = 0; i < NBK; ++i) {
-                    const float (&v)[4] = oacc[o * NBK + i];
-                    const int col = (o * NBK + i) * 8 + tq * 2;
-                    if (whole) {
-                        if (live0) *reinterpret_cast<uint32_t*>(p.out + orow0 * D + col) = pack_bf16(v[0] * inv0, v[1] * inv0);
-                        if (live1) *reinterpret_cast<uint32_t*>(p.out + orow1 * D + col) = pack_bf16(v[2] * inv1, v[3] * inv1);
-                    } else {
-                        if (live0) *reinterpret_cast<float2*>(po + (rg * 16 + quad) * D + col) = make_float2(v[0], v[1]);
-                        if (live1) *reinterpret_cast<float2*>(po + (rg * 16 + quad + 8) * D + col) = make_float2(v[2], v[3]);
-                    }
-                }
+            if (!c.finish(p, ti, kt, sm.ml + parity * KS * S::ROWS, warp, slot, merge_sync)) break;
+            parity ^= 1;                                       // (a warp may be a unit ahead of one that still reads its sums)
+            fence_proxy_async_smem();                          // (the next copy into this place is the producer's)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->empty[this_stage]);
+            // a shared unit's part has been written; who comes last is found out once, when this CTA has read all its tiles
+            if (ti.n_parts > 1) {
+                const int k = (ti.flags & TILE_END) ? 1 : 0;   // (in between units are whole)
+                if (threadIdx.x == 0) bars->shared_unit[k] = ti;
+                n_shared |= 1 << k;
             }
-            if (ks == 0 && tq == 0) {
-                if (whole) {
-                    if (p.lse != nullptr) {
-                        if (live0) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h0) * p.L + i0] = tm0 == -INFINITY ? -INFINITY : (tm0 + log2f(tl0)) * LN2_F;
-                        if (live1) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h1) * p.L + i1] = tm1 == -INFINITY ? -INFINITY : (tm1 + log2f(tl1)) * LN2_F;
-                    }
-                } else {
-                    float2* pm = reinterpret_cast<float2*>(p.part_ml) + static_cast<size_t>(slot) * ROWS + rg * 16 + quad;
-                    pm[0] = make_float2(tm0, tl0);
-                    pm[8] = make_float2(tm1, tl1);
-                }
-            }
-            if (!whole) {
-                // ---------------- the last of the unit's CTAs to come joins the parts, in the order of the keys
-                __threadfence();
+            if (!(ti.flags & TILE_END)) continue;
+            if (n_shared) {
                 if (!merge_sync()) break;
-                if (threadIdx.x == 0) {
-                    const uint32_t before = atomicAdd(&p.counters[ti.first_cta], 1u);
-                    bars->arrived = before;
-                    if (before == static_cast<uint32_t>(ti.n_parts) - 1) p.counters[ti.first_cta] = 0;      // for the next launch
-                    __threadfence();
+                if (threadIdx.x < 2 && (n_shared >> threadIdx.x & 1)) {
+                    const TileDesc& u = bars->shared_unit[threadIdx.x];
+                    const bool last = atomic_inc_acq_rel(&p.counters[u.first_cta]) == static_cast<uint32_t>(u.n_parts) - 1;
+                    bars->arrived[threadIdx.x] = last;
+                    if (last) p.counters[u.first_cta] = 0;         // for the next launch
                 }
                 if (!merge_sync()) break;
-                if (bars->arrived == static_cast<uint32_t>(ti.n_parts) - 1) {
-                    const int rows = min(ROWS, p.R - ti.chunk * ROWS);
-                    for (int item = threadIdx.x; item < rows * (D / 4); item += NCW * 32) {
-                        const int row = item / (D / 4), c4 = item % (D / 4);
-                        const float2* pm = reinterpret_cast<const float2*>(p.part_ml) + row;
-                        const float* px = p.part_o + row * D + c4 * 4;
-                        float m = -INFINITY, l = 0.f;
-                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int k = 0; k < ti.n_parts; ++k) {
-                            const size_t s = static_cast<size_t>(ti.first_cta + k) * 2 + (k == 0 ? ti.first_slot : 0);
-                            const float2 ml = __ldcg(pm + s * ROWS);
-                            const float4 x = ld_global_cg_f4(px + s * ROWS * D);
-                            const float mn = fmaxf(m, ml.x);
-                            const float wa = mn == -INFINITY ? 0.f : fast_exp2(m - mn), wb = mn == -INFINITY ? 0.f : fast_exp2(ml.x - mn);
-                            m = mn;
-                            l = l * wa + ml.y * wb;
-                            acc.x = acc.x * wa + x.x * wb; acc.y = acc.y * wa + x.y * wb;
-                            acc.z = acc.z * wa + x.z * wb; acc.w = acc.w * wa + x.w * wb;
-                        }
-                        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-                        const int rho = ti.chunk * ROWS + row, i = rho / p.g, h = ti.kvh * p.g + rho % p.g;
-                        const uint2 packed = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                        *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(ti.b) * p.L + i) * p.Hq + h) * D + c4 * 4) = packed;
-                        if (p.lse != nullptr && c4 == 0)
-                            p.lse[(static_cast<size_t>(ti.b) * p.Hq + h) * p.L + i] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * LN2_F;
-                    }
-                }
+                for (int k = 0; k < 2; ++k)
+                    if ((n_shared >> k & 1) && bars->arrived[k]) join_parts<D, S::ROWS, NCW * 32>(p, bars->shared_unit[k]);
             }
-            if (ti.flags & TILE_END) break;
+            break;
         }
     }
     // (the next kernel is let in late: its CTAs would pile up on the few SMs that have room beside this one's)
@@ -552,9 +844,10 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
 }
 
-// Row groups per CTA, by the packed query rows R of a (sequence, KV head): up to 16 rows four key slices share one, up to 32 two
-// share two, more take four row groups per chunk of 64 rows.
-int paged_row_groups(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }
+// Row groups per CTA, by the packed query rows R of a (sequence, KV head): up to 8 rows are the MMA's columns (0), up to 16 its
+// rows, four key slices each; up to 32 two groups of two slices; more take four groups per chunk of 64 rows.
+int paged_row_groups(int R) { return R <= 8 ? 0 : R <= 16 ? 1 : R <= 32 ? 2 : 4; }
+int paged_chunk_rows(int nw) { return nw == 0 ? 8 : nw * 16; }
 
 template <int D, int NW, int KS>
 int launch_paged(const dare_ctx* ctx, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const PagedParams& p, int ctas, cudaStream_t stream) {
@@ -562,7 +855,7 @@ int launch_paged(const dare_ctx* ctx, const CUtensorMap& tm_k, const CUtensorMap
     static_assert(2 * (S::SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
     static std::atomic<uint64_t> smem_set{0};
     if (ensure_dynamic_smem(smem_set, attn_paged_kernel<D, NW, KS>, S::SMEM) != DARE_OK) return DARE_ERR_CUDA;
-    return launch_kernel(attn_paged_kernel<D, NW, KS>, dim3(ctas), (NW * KS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
+    return launch_kernel(attn_paged_kernel<D, NW, KS>, dim3(ctas), (S::WARPS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -584,7 +877,8 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     PagedParams p = {};
     p.B = B; p.L = L; p.Hq = Hq; p.Hkv = Hkv; p.g = Hq / Hkv; p.R = L * p.g;
     const int nw = paged_row_groups(p.R);
-    p.chunks = (p.R + nw * 16 - 1) / (nw * 16);
+    const int rows = paged_chunk_rows(nw);
+    p.chunks = (p.R + rows - 1) / rows;
     p.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
     p.n_pages = n_pages; p.max_pages = max_pages;
     // a window that reaches further than any key is none (and keeps the kernel's sums within 32 bits)
@@ -597,10 +891,11 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     p.counters = ctx->join_counters; p.dev_status = ctx->dev_status;
     // two CTAs per SM, all resident at once; no more than there can be tiles
     const long long tiles = static_cast<long long>(B) * Hkv * p.chunks * ((static_cast<long long>(max_pages) * page_size + PG_KT - 1) / PG_KT);
+    if (tiles > (1LL << 30)) return DARE_ERR_SHAPE;
     long long ctas = 2LL * ctx->sm_count;
     if (ctas > PAGED_MAX_CTAS) ctas = PAGED_MAX_CTAS;
     if (ctas > tiles) ctas = tiles;
-    const size_t part_rows = static_cast<size_t>(ctas) * 2 * nw * 16;
+    const size_t part_rows = static_cast<size_t>(ctas) * 2 * rows;
     if (part_rows * (d + 2) * sizeof(float) > ctx->workspace_bytes) return DARE_ERR_WORKSPACE;
     p.part_o = static_cast<float*>(ctx->workspace);
     p.part_ml = p.part_o + part_rows * d;
@@ -613,8 +908,8 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int n = static_cast<int>(ctas);
     if (d == 128)
-        return nw == 1 ? launch_paged<128, 1, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 2 ? launch_paged<128, 2, 2>(ctx, tm_k, tm_v, p, n, s)
-                                                                                   : launch_paged<128, 4, 1>(ctx, tm_k, tm_v, p, n, s);
-    return nw == 1 ? launch_paged<64, 1, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 2 ? launch_paged<64, 2, 2>(ctx, tm_k, tm_v, p, n, s)
-                                                                              : launch_paged<64, 4, 1>(ctx, tm_k, tm_v, p, n, s);
+        return nw == 0 ? launch_paged<128, 0, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 1 ? launch_paged<128, 1, 4>(ctx, tm_k, tm_v, p, n, s)
+             : nw == 2 ? launch_paged<128, 2, 2>(ctx, tm_k, tm_v, p, n, s) : launch_paged<128, 4, 1>(ctx, tm_k, tm_v, p, n, s);
+    return nw == 0 ? launch_paged<64, 0, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 1 ? launch_paged<64, 1, 4>(ctx, tm_k, tm_v, p, n, s)
+         : nw == 2 ? launch_paged<64, 2, 2>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64, 4, 1>(ctx, tm_k, tm_v, p, n, s);
 }
