@@ -41,6 +41,10 @@ struct AttnParams {
     float* part_o;                // [splits][B*L*Hq][D] fp32, used when splits > 1
     float* part_lse;              // [splits][B*L*Hq]
     uint32_t* dev_status;
+    // keys in pages (tcgen05 kernel, PAGED): [n_pages, Hkv, page, D], the table [B, max_pages], keys per sequence
+    const int32_t *table, *kv_lens;
+    int page_shift, n_pages, max_pages;
+    int window, sinks;            // window 0: all keys
     int beside_head;              // inputs are ready although the kernels before this one still run (see enqueue_step)
 };
 
@@ -504,6 +508,7 @@ constexpr int TC_KT = 64;                 // keys per tile
 // 8 units 2.301, 2.223, 2.110, 1.851, 1.525; 4 units 2.300, 2.102, 1.865, 1.707, 1.469; 2 units 2.274, 1.944, 1.761, 1.669, 1.457, but the
 // ordinary scores of deviation 1 then move too (7 % on 32 sequences of 256 to 1024 tokens; 8 to 4 units: no difference).
 constexpr float TC_RESCALE_GAP = 4.0f;
+constexpr int PAGED_TC_LEAST = 4;         // tiles that are worth a part of a paged unit's keys
 
 template <int D, int QT>
 struct TcShape {
@@ -538,8 +543,16 @@ struct TcUnit {
     int token0;              // first token of the rollout / sequence in q and out
     int L_eff;               // block positions of the rollout / sequence
     int b, kvh;
-    int len_pre, len_blk, len_suf;
+    int len_pre, len_blk, len_suf;      // PAGED: keys of the sequence; the first that the unit's first query sees in its window; -
+    int t0, split;                      // PAGED: first of the sequence's tiles; which part of them this is
 };
+
+// Keys in pages: first key of the unit's tile t (the tiles of the first positions, then those from the window's first one on), and
+// the number of its tiles (at least 1, so that an empty sequence's rows are written).
+__device__ __forceinline__ int paged_sink_tiles(const AttnParams& p, int n, int first) {
+    return min(first / TC_KT, (min(p.sinks, n) + TC_KT - 1) / TC_KT);
+}
+__device__ __forceinline__ int paged_key0(int t, int n_sink, int first) { return (t < n_sink ? t : first / TC_KT + t - n_sink) * TC_KT; }
 
 template <int STAGES, int QT>
 struct TcBarriers {
@@ -556,7 +569,9 @@ struct TcBarriers {
     uint32_t abort_flag;
 };
 
-template <int D, int QT>
+// PAGED: the keys lie in the pages of a cache (tm_kpre, tm_vpre: the pool, a box per piece of a page), optionally seen through a sliding
+// window beside a few first positions (dare_attn_paged).
+template <int D, int QT, bool PAGED>
 __global__ void __launch_bounds__(TcShape<D, QT>::THREADS, 1)
 attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kpre,
                      const __grid_constant__ CUtensorMap tm_vpre, const __grid_constant__ CUtensorMap tm_kblk,
@@ -644,10 +659,86 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 TcUnit w;
                 w.b = static_cast<int>(y) / p.Hkv;
                 w.kvh = static_cast<int>(y) % p.Hkv;
-                w.pos0 = static_cast<int>(chunk) * QT * pos_per_tile;
+                if constexpr (PAGED) {                     // (the parts of a unit's keys run along x with its chunks)
+                    w.split = static_cast<int>(chunk) % p.splits;
+                    w.pos0 = static_cast<int>(chunk) / p.splits * QT * pos_per_tile;
+                } else {
+                    w.pos0 = static_cast<int>(chunk) * QT * pos_per_tile;
+                }
                 w.token0 = packed ? p.cu_seqlens[w.b] : w.b * p.L;
                 w.L_eff = packed ? p.cu_seqlens[w.b + 1] - w.token0 : p.L;
-                if (w.pos0 < w.L_eff) {                    // (packed: the grid is cut for the longest sequence)
+                if constexpr (PAGED) {
+                    const int cap = p.max_pages << p.page_shift, raw = p.kv_lens[w.b];
+                    int n = max(0, min(raw, cap));
+                    if (raw != n) atomicOr(p.dev_status, DEV_LEN_CLAMPED);
+                    const int first = p.window > 0 ? max(0, n - p.L + w.pos0 - p.window + 1) : 0;
+                    const int n_sink = paged_sink_tiles(p, n, first);
+                    const int n_all = n_sink + (n + TC_KT - 1) / TC_KT - first / TC_KT;
+                    w.t0 = static_cast<int>(static_cast<long long>(n_all) * w.split / p.splits);
+                    const int t_end = static_cast<int>(static_cast<long long>(n_all) * (w.split + 1) / p.splits);
+                    if (t_end == w.t0) n = 0;              // (no tile: one without keys stands for it, so that its rows are written)
+                    w.len_pre = n;
+                    w.len_blk = first;
+                    w.len_suf = 0;
+                    w.n_tiles = max(1, t_end - w.t0);
+                    w.n_q = min(QT, (w.L_eff - w.pos0 + pos_per_tile - 1) / pos_per_tile);
+                    const int slot = n_units & 1;
+                    if (!mbar_wait(&bars->unit_empty[slot], ((n_units >> 1) & 1) ^ 1, abort_flag)) break;
+                    bars->unit[slot] = w;
+                    mbar_arrive(&bars->unit_full[slot]);
+                    ++n_units;
+                    // a tile is up to four pieces of pages; their table entries are asked for a tile ahead
+                    const int pp_shift = min(p.page_shift, 6), rows_pp = 1 << pp_shift, pieces = TC_KT >> pp_shift;
+                    const int pool_rows = (p.n_pages * p.Hkv) << p.page_shift;
+                    int page[4] = {};
+                    auto visible = [&](int key) { return key < n && (key < p.sinks || key + rows_pp > first); };
+                    auto look_up = [&](int t) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = paged_key0(w.t0 + t, n_sink, first) + i * rows_pp;
+                            if (i < pieces && visible(key)) page[i] = p.table[static_cast<long long>(w.b) * p.max_pages + (key >> p.page_shift)];
+                        }
+                    };
+                    look_up(0);
+                    for (int t = 0; t < w.n_tiles; ++t, ++n_kv) {
+                        const int stage = n_kv % STAGES, key0 = paged_key0(w.t0 + t, n_sink, first);
+                        if (!mbar_wait(&bars->empty[stage], ((n_kv / STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+                        uint8_t* kdst = kv_s + stage * S::KV_STAGE;
+                        mbar_arrive_expect_tx(&bars->full[stage], 2 * KV_BYTES);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (i >= pieces) continue;
+                            const int key = key0 + i * rows_pp;
+                            int row = pool_rows;           // behind the pool: zeros
+                            if (visible(key)) {
+                                if (page[i] >= 0 && page[i] < p.n_pages)
+                                    row = ((page[i] * p.Hkv + w.kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                                else atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
+                            }
+#pragma unroll
+                            for (int h = 0; h < NHALF; ++h) {
+                                tma_load_2d(kdst + h * HALF_K + i * rows_pp * 128, &tm_kpre, &bars->full[stage], h * 64, row);
+                                tma_load_2d(kdst + KV_BYTES + h * HALF_K + i * rows_pp * 128, &tm_vpre, &bars->full[stage], h * 64, row);
+                            }
+                        }
+                        if (t + 1 < w.n_tiles) look_up(t + 1);
+                        if (t != 0) continue;
+#pragma unroll
+                        for (int j = 0; j < QT; ++j) {     // the Q tiles, as below
+                            if (j >= w.n_q || !ok) continue;
+                            ok = mbar_wait(&bars->q_empty[j], (n_qload[j] & 1) ^ 1, abort_flag);
+                            if (!ok) continue;
+                            ++n_qload[j];
+                            mbar_arrive_expect_tx(&bars->q_full[j], static_cast<uint32_t>(rows_in_tile) * D * 2);
+#pragma unroll
+                            for (int h = 0; h < NHALF; ++h)
+                                tma_load_3d(q_s + j * S::Q_BYTES + h * HALF_Q, &tm_q, &bars->q_full[j], h * 64, w.kvh * p.g,
+                                            w.token0 + w.pos0 + j * pos_per_tile);
+                        }
+                        if (!ok) break;
+                    }
+                    if (!ok) break;
+                } else if (w.pos0 < w.L_eff) {             // (packed: the grid is cut for the longest sequence)
                     int P = p.prefix_len ? p.prefix_len[w.b]
                                          : (p.uniform_P >= 0 ? p.uniform_P : (p.inplace ? p.prefix_cap - p.L : p.prefix_cap));
                     int Sx = p.has_suffix ? (p.suffix_len ? p.suffix_len[w.b] : p.suffix_cap) : 0;
@@ -835,8 +926,15 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // the loop, spilled: 243 -> 256 us on 32 sequences of 256 to 1024 tokens.)
             float m_ref = r < rows_in_tile && w.pos0 + j * pos_per_tile + ri < w.L_eff ? -INFINITY : INFINITY, l = 0.f;
             bool ok = true;
+            // (of the whole sequence: where a part has no tile, len_pre is 0 and every key hidden)
+            const int n_sink = PAGED ? paged_sink_tiles(p, w.len_pre, w.len_blk) : 0;
             for (int t = 0; t < w.n_tiles; ++t) {
-                const int valid = tile_info<TC_KT>(t, n_pre, n_blk, w.len_pre, w.len_blk, w.len_suf, 0, 0, 0).valid;
+                // (PAGED: `valid` keys from the tile's first on exist; those below `hidden` lie in front of this row's window,
+                // except the first `shown`)
+                const int key0 = PAGED ? paged_key0(w.t0 + t, n_sink, w.len_blk) : 0;
+                const int valid = PAGED ? w.len_pre - key0 : tile_info<TC_KT>(t, n_pre, n_blk, w.len_pre, w.len_blk, w.len_suf, 0, 0, 0).valid;
+                const int shown = PAGED ? p.sinks - key0 : 0;
+                const int hidden = PAGED && p.window > 0 ? w.len_pre - p.L + w.pos0 + j * pos_per_tile + ri - p.window + 1 - key0 : 0;
                 const uint32_t n = n_s + t;
                 const int buf = n & 1;
                 if (!mbar_wait(&bars->s_full[j][buf], (n >> 1) & 1, abort_flag)) { ok = false; break; }
@@ -853,6 +951,13 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         if (k + 32 >= valid) s1[k] = 0xff800000u;
                     }
                 }
+                if (PAGED && __any_sync(0xffffffffu, hidden > 0 && shown < TC_KT)) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        if (k < hidden && k >= shown) s0[k] = 0xff800000u;
+                        if (k + 32 < hidden && k + 32 >= shown) s1[k] = 0xff800000u;
+                    }
+                }
                 float t0 = max3(s0[0], s0[1], s0[2]), t1 = max3(s1[0], s1[1], s1[2]);
                 float t2 = max3(s0[3], s0[4], s0[5]), t3 = max3(s1[3], s1[4], s1[5]);
 #pragma unroll
@@ -866,11 +971,11 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 t1 = max3(__float_as_uint(t1), s1[30], s1[31]);
                 t0 = fmaxf(t0, t2);
                 t1 = fmaxf(t1, t3);
-                if (t == 0 && w.n_tiles > 1) {
+                if (t == 0 && w.n_tiles > 1 && !(PAGED && p.window > 0)) {
                     // The first reference is the largest score of 128 keys (the second tile's are on their way already): the oftener a
                     // row's largest weight is 1, the less its rounding to bf16 costs (scores of standard deviation 1 are 0.75 % further from
                     // 64 bits otherwise; it takes 2.5 % of 32 sequences of 256 to 1024 tokens, 5 to 10 of shorter ones).
-                    const int valid1 = tile_info<TC_KT>(1, n_pre, n_blk, w.len_pre, w.len_blk, w.len_suf, 0, 0, 0).valid;
+                    const int valid1 = PAGED ? w.len_pre - paged_key0(w.t0 + 1, n_sink, w.len_blk) : tile_info<TC_KT>(1, n_pre, n_blk, w.len_pre, w.len_blk, w.len_suf, 0, 0, 0).valid;
                     if (!mbar_wait(&bars->s_full[j][buf ^ 1], ((n + 1) >> 1) & 1, abort_flag)) { ok = false; break; }
                     tc_fence_after_sync();
 #pragma unroll 1
@@ -948,7 +1053,19 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_st_wait();
                 const float psum0 = __uint_as_float(static_cast<uint32_t>(psum)), psum1 = __uint_as_float(static_cast<uint32_t>(psum >> 32));
                 l += psum0 + psum1;
-                if (valid < TC_KT) {
+                if (PAGED) {
+                    // V rows that no query of the unit may see, as below
+                    const int first = p.window > 0 ? w.len_blk - key0 : 0;
+                    if (valid < TC_KT || (first > 0 && shown < TC_KT)) {
+                        uint8_t* vt = kv_s + (n_kv + t) % STAGES * S::KV_STAGE + KV_BYTES;
+                        for (int q = r; q < TC_KT * 8 * NHALF; q += 128) {
+                            const int k = (q >> 3) % TC_KT, h2 = (q >> 3) / TC_KT;
+                            if (k >= valid || (k < first && k >= shown))
+                                *reinterpret_cast<uint4*>(vt + h2 * HALF_K + k * 128 + (q & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                    }
+                } else if (valid < TC_KT) {
                     // V rows past the segment's end hold whatever lies behind it in memory: zero them so that
                     // probability 0 times garbage cannot make a NaN (thread r clears 16-byte pieces of those rows;
                     // both query tiles' warps do it, each before it releases its own second MMA)
@@ -972,6 +1089,28 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // and 32 lanes storing 16 bytes each to 32 different rows cost a request per lane): 64 columns at a time,
             // 16-byte chunk c of row r at c ^ (r & 7).
             const int pos0 = w.pos0 + j * pos_per_tile;
+            if (PAGED && p.splits > 1) {
+                // a part: fp32, each thread its row; attn_combine_kernel adds them up
+                const bool live = r < rows_in_tile && pos0 + ri < w.L_eff;
+                const size_t row = (static_cast<size_t>(w.token0) + pos0 + ri) * p.Hq + w.kvh * p.g + rh;
+                const size_t n_rows = static_cast<size_t>(p.B) * p.L * p.Hq;
+                float4* dst = reinterpret_cast<float4*>(p.part_o + (w.split * n_rows + row) * D);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t ov[32];
+                    tmem_ld_32cols(tm_o + c * 32, ov);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (live)
+                            dst[c * 8 + k] = make_float4(__uint_as_float(ov[4 * k]) * inv, __uint_as_float(ov[4 * k + 1]) * inv,
+                                                         __uint_as_float(ov[4 * k + 2]) * inv, __uint_as_float(ov[4 * k + 3]) * inv);
+                }
+                if (live) p.part_lse[w.split * n_rows + row] = l > 0.f ? (m_ref + log2f(l)) * LN2_F : -INFINITY;
+                __syncwarp();
+                tc_fence_before_sync();
+                continue;
+            }
 #pragma unroll
             for (int h2 = 0; h2 < NHALF; ++h2) {
                 uint32_t oa[32], ob[32];
@@ -1028,13 +1167,13 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (p.beside_head && has_last) pdl_wait();
 }
 
-template <int D, int QT>
+template <int D, int QT, bool PAGED = false>
 int launch_tc(const CUtensorMap& tm_q, const CUtensorMap* tm, const AttnParams& p, int q_tiles, cudaStream_t stream) {
     constexpr int SMEM = TcShape<D, QT>::SMEM;
     static std::atomic<uint64_t> smem_set{0};
-    if (ensure_dynamic_smem(smem_set, attn_block_tc_kernel<D, QT>, SMEM) != DARE_OK) return DARE_ERR_CUDA;
-    dim3 grid((q_tiles + QT - 1) / QT, p.B * p.Hkv, 1);
-    return launch_kernel(attn_block_tc_kernel<D, QT>, grid, TcShape<D, QT>::THREADS, SMEM, stream, 1, tm_q, tm[0], tm[1], tm[2],
+    if (ensure_dynamic_smem(smem_set, attn_block_tc_kernel<D, QT, PAGED>, SMEM) != DARE_OK) return DARE_ERR_CUDA;
+    dim3 grid((q_tiles + QT - 1) / QT * (PAGED ? p.splits : 1), p.B * p.Hkv, 1);
+    return launch_kernel(attn_block_tc_kernel<D, QT, PAGED>, grid, TcShape<D, QT>::THREADS, SMEM, stream, 1, tm_q, tm[0], tm[1], tm[2],
                          tm[3], tm[4], tm[5], p);
 }
 
@@ -1079,6 +1218,14 @@ __global__ void attn_combine_kernel(const float* __restrict__ part_o, const floa
         const size_t h = row % Hq, bi = row / Hq, i = bi % L, bb = bi / L;
         lse[(bb * Hq + h) * L + i] = wsum > 0.f ? mx + logf(wsum) : -INFINITY;
     }
+}
+
+int launch_combine(const AttnParams& p, size_t n_rows, int d, cudaStream_t stream) {
+    const int tpr = d / 4;                    // threads per row
+    const int rows_per_block = 256 / tpr;
+    const unsigned blocks = static_cast<unsigned>((n_rows + rows_per_block - 1) / rows_per_block);
+    return launch_kernel(d == 128 ? attn_combine_kernel<128> : attn_combine_kernel<64>, dim3(blocks), 256, 0, stream, 1,
+                         p.part_o, p.part_lse, p.splits, n_rows, p.L, p.Hq, p.out, p.lse);
 }
 
 template <int D, int NW, int KS, int KT, int STAGES, int CPS>
@@ -1136,7 +1283,7 @@ size_t attn_workspace_bytes(const AttnArgs& a, int splits) {
 }
 
 int launch_attn(const dare_ctx* ctx, const AttnArgs& a, cudaStream_t stream) {
-    AttnParams p;
+    AttnParams p = {};
     p.B = a.B; p.L = a.L; p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = a.Hq / a.Hkv; p.R = a.L * p.g;
     p.prefix_cap = a.prefix_cap; p.suffix_cap = a.k_suf ? a.suffix_cap : 0;
     p.inplace = a.k_blk == nullptr; p.has_suffix = a.k_suf != nullptr && a.suffix_cap > 0;
@@ -1199,13 +1346,7 @@ int launch_attn(const dare_ctx* ctx, const AttnArgs& a, cudaStream_t stream) {
                      : launch_one<64, 4, 1, 64, 3, 2>(tm, p, chunks, stream);
     }
     if (rc != DARE_OK) return rc;
-    if (p.splits > 1) {
-        const int tpr = a.d / 4;                    // threads per row
-        const int rows_per_block = 256 / tpr;
-        const unsigned blocks = static_cast<unsigned>((n_rows + rows_per_block - 1) / rows_per_block);
-        return launch_kernel(a.d == 128 ? attn_combine_kernel<128> : attn_combine_kernel<64>, dim3(blocks), 256, 0, stream, 1,
-                             p.part_o, p.part_lse, p.splits, n_rows, a.L, a.Hq, p.out, p.lse);
-    }
+    if (p.splits > 1) return launch_combine(p, n_rows, a.d, stream);
     return DARE_OK;
 }
 
@@ -1236,6 +1377,46 @@ int launch_attn_varlen(const dare_ctx* ctx, int total, int n_seqs, int max_seqle
     if (rc != DARE_OK) return rc;
     if (q_tiles >= 2) return d == 128 ? launch_tc<128, 2>(tm_q, tm, p, q_tiles, stream) : launch_tc<64, 2>(tm_q, tm, p, q_tiles, stream);
     return d == 128 ? launch_tc<128, 1>(tm_q, tm, p, q_tiles, stream) : launch_tc<64, 1>(tm_q, tm, p, q_tiles, stream);
+}
+
+// The paged form of the tcgen05 kernel (dare_attn_paged, where many query rows share a KV head).
+int launch_attn_paged_tc(const dare_ctx* ctx, const PagedAttnArgs& a, cudaStream_t stream) {
+    AttnParams p = {};
+    p.B = a.B; p.L = a.L; p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = a.Hq / a.Hkv; p.R = a.L * p.g;
+    p.uniform_P = -1;
+    p.scale_log2 = a.scale * LOG2E_F;
+    p.q = static_cast<const __nv_bfloat16*>(a.q);
+    p.out = static_cast<__nv_bfloat16*>(a.out); p.lse = a.lse;
+    p.dev_status = ctx->dev_status;
+    p.table = a.table; p.kv_lens = a.kv_lens; p.page_shift = a.page_shift; p.n_pages = a.n_pages; p.max_pages = a.max_pages;
+    p.window = a.window; p.sinks = a.sinks;
+    const int pos_per_tile = 128 / p.g, q_tiles = (p.L + pos_per_tile - 1) / pos_per_tile;
+    // two query tiles per CTA where the CTAs still fill the SMs, as in launch_attn; where one tile's do not, the keys are cut too, into as
+    // many parts as keep the launch in one wave, of PAGED_TC_LEAST tiles at least where the table is filled
+    const long long pairs = static_cast<long long>((q_tiles + 1) / 2) * p.B * p.Hkv;
+    const bool two = q_tiles >= 2 && 4 * pairs >= 3LL * ctx->sm_count;
+    const long long units = static_cast<long long>(q_tiles) * p.B * p.Hkv;
+    const size_t n_rows = static_cast<size_t>(a.B) * a.L * a.Hq;
+    long long cap = static_cast<long long>(a.max_pages) << a.page_shift;
+    if (a.window > 0 && cap > static_cast<long long>(a.window) + a.L + a.sinks) cap = static_cast<long long>(a.window) + a.L + a.sinks;
+    long long splits = ctx->sm_count / units;
+    if (splits > cap / (PAGED_TC_LEAST * TC_KT)) splits = cap / (PAGED_TC_LEAST * TC_KT);
+    if (splits > static_cast<long long>(ctx->workspace_bytes / (n_rows * (a.d + 1) * sizeof(float)))) splits = 1;
+    p.splits = two || splits < 2 ? 1 : static_cast<int>(splits);
+    p.part_o = static_cast<float*>(ctx->workspace);
+    p.part_lse = p.part_o + static_cast<size_t>(p.splits) * n_rows * a.d;
+    const uint64_t pool_rows = (static_cast<uint64_t>(a.n_pages) * a.Hkv) << a.page_shift;
+    const uint32_t box = a.page_shift < 6 ? 1u << a.page_shift : TC_KT;
+    CUtensorMap tm_q, tm[6];
+    int rc = make_tmap_bf16_2d(ctx, &tm[0], a.k_pages, pool_rows, a.d, box, 64);
+    if (rc == DARE_OK) rc = make_tmap_bf16_2d(ctx, &tm[1], a.v_pages, pool_rows, a.d, box, 64);
+    if (rc == DARE_OK) rc = make_tmap_bf16_3d(ctx, &tm_q, a.q, static_cast<uint64_t>(a.B) * a.L, a.Hq, a.d, pos_per_tile, p.g, 64);
+    if (rc != DARE_OK) return rc;
+    tm[2] = tm[0]; tm[3] = tm[1]; tm[4] = tm[0]; tm[5] = tm[1];
+    if (two) return a.d == 128 ? launch_tc<128, 2, true>(tm_q, tm, p, q_tiles, stream) : launch_tc<64, 2, true>(tm_q, tm, p, q_tiles, stream);
+    rc = a.d == 128 ? launch_tc<128, 1, true>(tm_q, tm, p, q_tiles, stream) : launch_tc<64, 1, true>(tm_q, tm, p, q_tiles, stream);
+    if (rc != DARE_OK || p.splits == 1) return rc;
+    return launch_combine(p, n_rows, a.d, stream);
 }
 
 }  // namespace dare

@@ -207,6 +207,18 @@ int launch_attn_varlen(const dare_ctx* ctx, int total, int n_seqs, int max_seqle
                        const void* q, const void* k, const void* v, const int32_t* cu_seqlens, void* out, float* lse,
                        cudaStream_t stream);
 
+// Attention over a paged cache, arguments checked and completed (paged.cu): scale > 0, page size 1 << page_shift, a window that
+// hides nothing is 0.
+struct PagedAttnArgs {
+    int B, L, Hq, Hkv, d, page_shift, n_pages, max_pages, window, sinks;
+    float scale;
+    const void *q, *k_pages, *v_pages;
+    const int32_t *table, *kv_lens;
+    void* out;
+    float* lse;
+};
+int launch_attn_paged_tc(const dare_ctx* ctx, const PagedAttnArgs& a, cudaStream_t stream);
+
 // ---- layer stack (gemm.cu, layers.cu)
 enum { GEMM_EPI_STORE = 0, GEMM_EPI_RESIDUAL = 1, GEMM_EPI_SWIGLU = 2, GEMM_EPI_ROPE = 3 };
 // out[M, N] = epilogue(a[M, K] . w[N, K]^T), bf16 row-major, ldo = elements per output row.

@@ -4,19 +4,19 @@
 //
 // What bounds it is reading K and V once (4 d Hkv bytes per key against 4 d Hq L flops), so the kernel is organised around that
 // stream:
-//   * the work is cut by keys, not by sequences: the 64-key tiles of all (sequence, KV head, chunk of query rows) units are one
+//   * the work is cut by keys, not by sequences: the 64-key tiles of all (sequence, KV head) units are one
 //     list, and each of the CTAs that the GPU holds at once takes an equal stretch of it.  A single long sequence, a full batch
 //     and a ragged one all keep every SM reading until the end.  A unit that lies in several stretches is joined by whichever
 //     of its CTAs comes last, in the order of the keys, so that results do not depend on the order of arrival;
-//   * the query rows of all Hq / Hkv heads that share a KV head are one tile: a key is read once for them;
-//   * a producer warp looks up pages two tiles ahead and streams the tiles through a shared-memory ring with TMA (128-byte
+//   * the query rows of all Hq / Hkv heads that share a KV head are one tile of up to 8: a key is read once for them.  (More rows
+//     go to the tcgen05 kernel of attn.cu, see launch_attn_paged_tc);
+//   * a producer warp copies table entries two tiles ahead and streams the tiles through a shared-memory ring with TMA (128-byte
 //     swizzle; a lane per page piece; pieces that nobody may see are read at a row behind the pool, which TMA fills with zeros);
-//   * consumer warps own 16 query rows and, where few rows share a KV head, a slice of each tile's keys: QK^T and PV on
-//     warp-level MMAs (m16n8k16), the online softmax in registers.
+//   * four consumer warps own 16 keys of each tile: QK^T and PV on warp-level MMAs (m16n8k16) with the keys and channels as rows and
+//     the query rows as columns, the online softmax in registers.
 // Probabilities are rounded to bf16 for the second product (relative 2^-9, averaged over the keys); maximum, sum, products and
 // the joined parts are fp32; the output is rounded once.
 #include <math.h>
-#include <type_traits>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -28,11 +28,13 @@ constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr float LN2_F = 0.6931471805599453f;
 
 constexpr int PG_KT = 64;          // keys per tile
+constexpr int PG_ROWS = 8;         // packed query rows of a unit, at most
+constexpr int PG_WARPS = 4;        // consumers, each with 16 of a tile's keys
 constexpr int PG_LEAST = 3;        // tiles that are a CTA's worth
 constexpr int PG_AHEAD = 2;        // tiles whose pages are looked up before their turn
 
 struct PagedParams {
-    int B, L, Hq, Hkv, g, R, chunks;      // R = L * g packed query rows per (sequence, KV head), in `chunks` of NW * 16
+    int B, L, Hq, Hkv, g, R;              // R = L * g packed query rows per (sequence, KV head)
     int page_shift, n_pages, max_pages;
     int window, sinks;                    // window 0: all keys
     float scale_log2;
@@ -40,8 +42,8 @@ struct PagedParams {
     const int32_t *table, *kv_lens;
     __nv_bfloat16* out;
     float* lse;
-    float* part_o;                        // [CTAs][2][NW * 16][D]: a CTA's first and last unit, where others share them
-    float* part_ml;                       // [CTAs][2][NW * 16][2]: maximum (log2 domain) and sum
+    float* part_o;                        // [CTAs][2][PG_ROWS][D]: a CTA's first and last unit, where others share them
+    float* part_ml;                       // [CTAs][2][PG_ROWS][2]: maximum (log2 domain) and sum
     uint32_t* counters;
     uint32_t* dev_status;
 };
@@ -51,7 +53,7 @@ enum { TILE_FIRST = 1, TILE_LAST = 2, TILE_END = 4, TILE_MASKED = 8, TILE_NONE =
 // A tile, as the producer hands it to the consumers.
 struct TileDesc {
     int flags;                // TILE_*: first / last of its unit in this CTA, last of the CTA, some row must not see some key
-    int b, kvh, chunk;
+    int b, kvh;
     int key0, n;              // first key, keys of the sequence
     int first_cta, n_parts;   // the CTAs that share the unit
     int first_slot;           // the slot of first_cta's part
@@ -69,21 +71,15 @@ struct PagedBarriers {
     uint32_t arrived[2];
 };
 
-// NW row groups of 16 packed query rows; KS warps share a row group and split every tile's keys between them.  NW = 0: at most 8
-// rows, four key slices (see FewRows).
-template <int D, int NW, int KS>
+template <int D>
 struct PagedShape {
-    static constexpr bool FEW = NW == 0;
-    static constexpr int ROWS = FEW ? 8 : NW * 16;
-    static constexpr int WARPS = FEW ? KS : NW * KS;                                  // consumers
     static constexpr int STAGE = 2 * PG_KT * D * 2;
     static constexpr int STAGES = D == 128 ? 3 : 6;
-    static constexpr int ML = 2 * KS * ROWS * 8;                                      // [unit's parity][KS][ROWS] maximum and sum
+    static constexpr int ML = 2 * PG_WARPS * PG_ROWS * 8;                             // [unit's parity][slice][row] maximum and sum
     // Query rows arrive with their unit's first tile, where there is room for them in each of the ring's places; rows are 16 bytes
     // apart from a power of two (ldmatrix without bank conflicts).
-    static constexpr bool Q_SMEM = ROWS <= 16;
     static constexpr int Q_ROW = D * 2 + 16;
-    static constexpr int Q_STAGE = Q_SMEM ? ROWS * Q_ROW : 0;
+    static constexpr int Q_STAGE = PG_ROWS * Q_ROW;
     static constexpr int SMEM = STAGES * (STAGE + Q_STAGE) + ML + static_cast<int>(sizeof(PagedBarriers<STAGES>)) + 1024;
 };
 
@@ -127,10 +123,11 @@ __device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINI
 // Adds a unit's parts up, in the order of the keys (the order of arrival does not show).  A thread has four channels of a row,
 // two rows at once, and asks for JOIN parts at a time: what this costs is trips to L2, one after the other.
 constexpr int JOIN = 8;
-template <int D, int ROWS, int THREADS>
+template <int D>
 __device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc& unit) {
+    constexpr int THREADS = PG_WARPS * 32;
     const TileDesc u = unit;
-    const int items = min(ROWS, p.R - u.chunk * ROWS) * (D / 4);
+    const int items = p.R * (D / 4);
     const float2* part_ml = reinterpret_cast<const float2*>(p.part_ml);
     const float4* part_o = reinterpret_cast<const float4*>(p.part_o);
     for (int item0 = threadIdx.x; item0 < items; item0 += 2 * THREADS) {
@@ -145,7 +142,7 @@ __device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc&
                 const int slot = (u.first_cta + part) * 2 + (part == 0 ? u.first_slot : 0);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int item = min(item0 + e * THREADS, items - 1), at = slot * ROWS + item / (D / 4);
+                    const int item = min(item0 + e * THREADS, items - 1), at = slot * PG_ROWS + item / (D / 4);
                     ml[e][k] = __ldcg(part_ml + at);
                     x[e][k] = __ldcg(part_o + static_cast<size_t>(at) * (D / 4) + item % (D / 4));
                 }
@@ -174,7 +171,7 @@ __device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc&
             const int item = item0 + e * THREADS;
             if (item >= items) continue;
             const float inv = inverse_sum(l[e]);
-            const int rho = u.chunk * ROWS + item / (D / 4), c4 = item % (D / 4), i = rho / p.g, h = u.kvh * p.g + rho - i * p.g;
+            const int rho = item / (D / 4), c4 = item % (D / 4), i = rho / p.g, h = u.kvh * p.g + rho - i * p.g;
             *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(u.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
                 make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
             if (p.lse != nullptr && c4 == 0)
@@ -184,10 +181,10 @@ __device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc&
 }
 
 // Shared memory of a CTA.
-template <int D, int NW, int KS>
+template <int D>
 struct PagedSmem {
-    using S = PagedShape<D, NW, KS>;
-    uint8_t *tiles, *q;                    // [STAGES][STAGE], [STAGES][ROWS][Q_ROW]
+    using S = PagedShape<D>;
+    uint8_t *tiles, *q;                    // [STAGES][STAGE], [STAGES][PG_ROWS][Q_ROW]
     float2* ml;
     PagedBarriers<S::STAGES>* bars;
     __device__ __forceinline__ explicit PagedSmem(uint8_t* raw) {
@@ -198,16 +195,15 @@ struct PagedSmem {
     }
 };
 
-// The producer warp: finds this CTA's stretch of the list of tiles (sequence by sequence, in it KV head by KV head, in that chunk
-// by chunk of the query rows) and sends for its tiles.
-template <int D, int NW, int KS>
-__device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorMap* tm_v, const PagedParams& p, const PagedSmem<D, NW, KS>& sm) {
-    using S = PagedShape<D, NW, KS>;
+// The producer warp: finds this CTA's stretch of the list of tiles (sequence by sequence, in it KV head by KV head) and sends for
+// its tiles.
+template <int D>
+__device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorMap* tm_v, const PagedParams& p, const PagedSmem<D>& sm) {
+    using S = PagedShape<D>;
     constexpr int STAGES = S::STAGES, HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2;
     PagedBarriers<STAGES>* bars = sm.bars;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int lane = threadIdx.x & 31;
-    const int HC = p.Hkv * p.chunks;
     int total = 0, lens = 0;                       // (lens, lane i: keys of sequence (b & ~31) + i)
     for (int b0 = (p.B - 1) & ~31; b0 >= 0; b0 -= 32) {
         lens = 0;
@@ -220,7 +216,7 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         }
         total += __reduce_add_sync(0xffffffffu, nt);
     }
-    const Stretches st(total * HC, p.B * HC, gridDim.x);
+    const Stretches st(total * p.Hkv, p.B * p.Hkv, gridDim.x);
     const int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
     if (begin >= end) {
         if (lane == 0) {
@@ -239,33 +235,33 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             const int o = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += o;
         }
-        const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * HC > begin);
+        const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * p.Hkv > begin);
         if (beyond) {
             const int i = __ffs(beyond) - 1;
             b = b0 + i;
-            base += __shfl_sync(0xffffffffu, incl - nt, i) * HC;
+            base += __shfl_sync(0xffffffffu, incl - nt, i) * p.Hkv;
             break;
         }
-        base += __shfl_sync(0xffffffffu, incl, 31) * HC;
+        base += __shfl_sync(0xffffffffu, incl, 31) * p.Hkv;
     }
     // two cursors over the tiles: `ahead` asks for table entries, `now` follows with the copies
     struct Cursor {
-        int b, u, t, base, lens;
+        int b, kvh, t, base, lens;
         SeqTiles sq;
-        __device__ __forceinline__ void next(const PagedParams& p, int HC, int lane) {
+        __device__ __forceinline__ void next(const PagedParams& p, int lane) {
             if (++t < sq.n_tiles) return;
             t = 0;
-            if (++u < HC) return;
-            u = 0;
-            base += sq.n_tiles * HC;
+            if (++kvh < p.Hkv) return;
+            kvh = 0;
+            base += sq.n_tiles * p.Hkv;
             ++b;
             if ((b & 31) == 0) lens = b + lane < p.B ? seq_keys(p, b + lane) : 0;
             if (b < p.B) sq = SeqTiles(__shfl_sync(0xffffffffu, lens, b & 31), p);
         }
     };
     const SeqTiles sq0(__shfl_sync(0xffffffffu, lens, b & 31), p);
-    const int u_begin = (begin - base) / sq0.n_tiles;
-    Cursor now = {b, u_begin, begin - base - u_begin * sq0.n_tiles, base, lens, sq0};
+    const int first_head = (begin - base) / sq0.n_tiles;
+    Cursor now = {b, first_head, begin - base - first_head * sq0.n_tiles, base, lens, sq0};
     Cursor ahead = now;
 
     // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of one half of K or V
@@ -282,21 +278,17 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             const int key = ahead.sq.key0(ahead.t) + piece * rows_pp;
             if (active && visible(ahead, key))
                 cp_async_4(&bars->pages[at % (PG_AHEAD + 2)][lane], p.table + static_cast<long long>(ahead.b) * p.max_pages + (key >> p.page_shift));
-            ahead.next(p, HC, lane);
+            ahead.next(p, lane);
         }
         cp_async_commit();
     };
 #pragma unroll
     for (int k = 0; k < PG_AHEAD; ++k) fetch(begin + k);
-    int stage = 0, kvh = 0, chunk = 0, c0 = 0, n_parts = 0, slot0 = 0;
+    int stage = 0, c0 = 0, n_parts = 0, slot0 = 0;
     uint32_t phase = 0;
     for (int at = begin; at < end; ++at) {
         fetch(at + PG_AHEAD);
         const bool first = now.t == 0 || at == begin;
-        if (first) {
-            kvh = p.chunks == 1 ? now.u : now.u / p.chunks;
-            chunk = now.u - kvh * p.chunks;
-        }
         if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag))) break;
         uint64_t* full = &bars->full[stage];
         const int key0 = now.sq.key0(now.t), key = key0 + piece * rows_pp;
@@ -305,7 +297,7 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             int row = pool_rows;                   // behind the pool: zeros
             if (visible(now, key)) {
                 const int page = bars->pages[at % (PG_AHEAD + 2)][lane];
-                if (page >= 0 && page < p.n_pages) row = ((page * p.Hkv + kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                if (page >= 0 && page < p.n_pages) row = ((page * p.Hkv + now.kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
                 else atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
             }
             // (the bytes may arrive before they are expected: the phase ends with the arrival below)
@@ -313,14 +305,12 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         }
         uint32_t bytes = 2 * KV_BYTES;
         if (first) {
-            if (S::Q_SMEM) {                       // (one chunk: packed query rows 0 .. R - 1 of the sequence)
-                if (lane < p.R) {
-                    const int i = lane / p.g, h = kvh * p.g + lane - i * p.g;
-                    bulk_load(sm.q + stage * S::Q_STAGE + lane * S::Q_ROW, p.q + ((static_cast<size_t>(now.b) * p.L + i) * p.Hq + h) * D, D * 2, full);
-                }
-                bytes += p.R * D * 2;
+            if (lane < p.R) {
+                const int i = lane / p.g, h = now.kvh * p.g + lane - i * p.g;
+                bulk_load(sm.q + stage * S::Q_STAGE + lane * S::Q_ROW, p.q + ((static_cast<size_t>(now.b) * p.L + i) * p.Hq + h) * D, D * 2, full);
             }
-            const int u0 = now.base + now.u * now.sq.n_tiles;
+            bytes += p.R * D * 2;
+            const int u0 = now.base + now.kvh * now.sq.n_tiles;
             c0 = st.cta_of(u0);
             n_parts = st.cta_of(u0 + now.sq.n_tiles - 1) - c0 + 1;
             slot0 = st.begin(c0) == u0 ? 0 : 1;
@@ -330,13 +320,13 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             TileDesc d;
             d.flags = (first ? TILE_FIRST : 0) | (now.t == now.sq.n_tiles - 1 || at == end - 1 ? TILE_LAST : 0) | (at == end - 1 ? TILE_END : 0);
             if (key0 + PG_KT > n || (p.window > 0 && key0 < n - p.window && key0 + PG_KT > p.sinks)) d.flags |= TILE_MASKED;
-            d.b = now.b; d.kvh = kvh; d.chunk = chunk; d.key0 = key0; d.n = n;
+            d.b = now.b; d.kvh = now.kvh; d.key0 = key0; d.n = n;
             d.first_cta = c0; d.n_parts = n_parts; d.first_slot = slot0;
             bars->tile[stage] = d;
             mbar_arrive_expect_tx(full, bytes);
         }
         __syncwarp();
-        now.next(p, HC, lane);
+        now.next(p, lane);
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
     }
 }
@@ -364,23 +354,23 @@ __device__ __forceinline__ void clear_unseen(const PagedParams& p, const TileDes
 // A consumer warp's state for up to 8 query rows: the products are turned round, S^T = K Q^T and O^T = V^T P^T, so that the rows
 // are the MMA's 8 columns and half as many MMAs and registers are needed as with rows for its 16.  Lane (quad, tq): keys (and
 // channels) quad and quad + 8 of each 16, query rows 2 tq and 2 tq + 1.  A warp owns 16 keys of each tile.
-template <int D, int KS>
+template <int D>
 struct FewRows {
-    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KPW = PG_KT / KS;
-    static_assert(KPW == 16, "a slice is one MMA's keys");
+    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KS = PG_WARPS, KPW = PG_KT / KS;
+    static_assert(KPW == 16 && PG_ROWS == 8, "a slice is one MMA's keys, the rows are its columns");
     uint32_t qb[D / 16][2];
     float o[D / 16][4];
     float m[2], l[2];
     int row_i[2];              // block positions of this lane's two rows
 
-    __device__ __forceinline__ void place(const PagedParams& p, int) {
+    __device__ __forceinline__ explicit FewRows(const PagedParams& p) {
         const int tq = threadIdx.x & 3;
         row_i[0] = p.L == 1 ? 0 : 2 * tq / p.g;
         row_i[1] = p.L == 1 ? 0 : (2 * tq + 1) / p.g;
     }
-    __device__ __forceinline__ void first(const PagedParams&, const TileDesc&, const uint8_t* q_rows, int q_row_bytes, int) {
+    __device__ __forceinline__ void first(const uint8_t* q_rows) {
         const int lane = threadIdx.x & 31;
-        const uint32_t qa = smem_u32(q_rows) + (lane & 7) * q_row_bytes + (lane >> 3) * 16;
+        const uint32_t qa = smem_u32(q_rows) + (lane & 7) * PagedShape<D>::Q_ROW + (lane >> 3) * 16;
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) ldmatrix_x4(qa + j * 64, qb[2 * j][0], qb[2 * j][1], qb[2 * j + 1][0], qb[2 * j + 1][1]);
 #pragma unroll
@@ -514,246 +504,13 @@ struct FewRows {
     }
 };
 
-// A consumer warp's state for 16 query rows (the MMA's rows) and 64 / KS of each tile's keys.  Lane (quad, tq): rows quad and
-// quad + 8, keys (and channels) 2 tq and 2 tq + 1 of each 8.
-template <int D, int NW, int KS>
-struct ManyRows {
-    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KPW = PG_KT / KS, ROWS = NW * 16;
-    static constexpr int NBK = D / 8 / KS;       // blocks of 8 columns that a warp finishes
-    static constexpr bool Q_SMEM = PagedShape<D, NW, KS>::Q_SMEM;
-    static_assert(KS * (KS - 1) * NW * NBK * 512 <= PagedShape<D, NW, KS>::STAGE, "the merge goes through the last tile's place in the ring");
-    uint32_t qf[D / 16][4];
-    float oacc[D / 8][4];
-    float m0, m1, l0, l1;
-    int i0, i1, g0, g1;                          // block positions of this lane's two rows, and heads within the group
-    bool live0, live1;
-
-    __device__ __forceinline__ void place(const PagedParams& p, int warp, int chunk = 0) {
-        const int rho0 = chunk * ROWS + warp % NW * 16 + ((threadIdx.x & 31) >> 2), rho1 = rho0 + 8;
-        live0 = rho0 < p.R;
-        live1 = rho1 < p.R;
-        i0 = live0 ? rho0 / p.g : 0;
-        i1 = live1 ? rho1 / p.g : 0;
-        g0 = live0 ? rho0 - i0 * p.g : 0;
-        g1 = live1 ? rho1 - i1 * p.g : 0;
-    }
-    __device__ __forceinline__ void first(const PagedParams& p, const TileDesc& ti, const uint8_t* q_rows, int q_row_bytes, int warp) {
-        const int lane = threadIdx.x & 31, tq = lane & 3;
-        if (Q_SMEM) {
-            const uint32_t qa = smem_u32(q_rows) + (lane & 15) * q_row_bytes + (lane >> 4) * 16;
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) ldmatrix_x4(qa + kk * 32, qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3]);
-        } else {
-            place(p, warp, ti.chunk);
-            const uint32_t* q0 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + ti.kvh * p.g + g0) * D);
-            const uint32_t* q1 = reinterpret_cast<const uint32_t*>(p.q + ((static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + ti.kvh * p.g + g1) * D);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                qf[kk][0] = live0 ? q0[kk * 8 + tq] : 0u;
-                qf[kk][1] = live1 ? q1[kk * 8 + tq] : 0u;
-                qf[kk][2] = live0 ? q0[kk * 8 + 4 + tq] : 0u;
-                qf[kk][3] = live1 ? q1[kk * 8 + 4 + tq] : 0u;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) oacc[n][0] = oacc[n][1] = oacc[n][2] = oacc[n][3] = 0.f;
-        m0 = m1 = -INFINITY;
-        l0 = l1 = 0.f;
-    }
-    __device__ __forceinline__ void tile(const PagedParams& p, const TileDesc& ti, uint8_t* kt, int warp) {
-        const int lane = threadIdx.x & 31, tq = lane & 3, mi = lane >> 3, rin = lane & 7, koff = warp / NW * KPW;
-        uint8_t* vt = kt + KV_BYTES;
-        const uint32_t kbase = smem_u32(kt), vbase = smem_u32(vt);
-        const float c = p.scale_log2;
-        const bool masked = ti.flags & TILE_MASKED;
-        if (masked) clear_unseen<KPW, NHALF>(p, ti, vt, koff);
-        // S = Q K^T for this warp's keys
-        float sacc[KPW / 8][4];
-#pragma unroll
-        for (int nb = 0; nb < KPW / 8; ++nb) sacc[nb][0] = sacc[nb][1] = sacc[nb][2] = sacc[nb][3] = 0.f;
-#pragma unroll
-        for (int kq = 0; kq < D / 32; ++kq) {
-            uint32_t kf[KPW / 8][4];
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) {
-                const int key = koff + nb * 8 + rin, ch = 4 * kq + mi;
-                ldmatrix_x4(kbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), kf[nb][0], kf[nb][1], kf[nb][2], kf[nb][3]);
-            }
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq], kf[nb][0], kf[nb][1]);
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) mma_bf16_16816(sacc[nb], qf[2 * kq + 1], kf[nb][2], kf[nb][3]);
-        }
-        if (masked) {
-            const int start = window_start(p, ti.n);
-#pragma unroll
-            for (int nb = 0; nb < KPW / 8; ++nb) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = ti.key0 + koff + nb * 8 + tq * 2 + (e & 1);
-                    if (key >= ti.n || (key >= p.sinks && key < start + (e < 2 ? i0 : i1))) sacc[nb][e] = -INFINITY;
-                }
-            }
-        }
-        float tmax0 = -INFINITY, tmax1 = -INFINITY;
-#pragma unroll
-        for (int nb = 0; nb < KPW / 8; ++nb) {
-            tmax0 = fmaxf(tmax0, fmaxf(sacc[nb][0], sacc[nb][1]));
-            tmax1 = fmaxf(tmax1, fmaxf(sacc[nb][2], sacc[nb][3]));
-        }
-        tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 1));
-        tmax0 = fmaxf(tmax0, __shfl_xor_sync(0xffffffffu, tmax0, 2));
-        tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 1));
-        tmax1 = fmaxf(tmax1, __shfl_xor_sync(0xffffffffu, tmax1, 2));
-        // (a row may have seen nothing yet: its reference is then 0, its weights exp2(-inf) = 0)
-        const float mn0 = fmaxf(m0, tmax0), mn1 = fmaxf(m1, tmax1);
-        const float r0 = mn0 == -INFINITY ? 0.f : mn0 * c, r1 = mn1 == -INFINITY ? 0.f : mn1 * c;
-        const bool moved = __any_sync(0xffffffffu, mn0 != m0 || mn1 != m1);
-        float ps0 = 0.f, ps1 = 0.f;
-        uint32_t pa[KPW / 16][4];
-#pragma unroll
-        for (int nb = 0; nb < KPW / 8; ++nb) {
-            const float e0 = fast_exp2(fmaf(sacc[nb][0], c, -r0)), e1 = fast_exp2(fmaf(sacc[nb][1], c, -r0));
-            const float e2 = fast_exp2(fmaf(sacc[nb][2], c, -r1)), e3 = fast_exp2(fmaf(sacc[nb][3], c, -r1));
-            ps0 += e0 + e1;
-            ps1 += e2 + e3;
-            pa[nb >> 1][(nb & 1) * 2 + 0] = pack_bf16(e0, e1);
-            pa[nb >> 1][(nb & 1) * 2 + 1] = pack_bf16(e2, e3);
-        }
-        if (moved) {
-            const float a0 = fast_exp2(fmaf(m0, c, -r0)), a1 = fast_exp2(fmaf(m1, c, -r1));
-            m0 = mn0;
-            m1 = mn1;
-            l0 *= a0;
-            l1 *= a1;
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n) {
-                oacc[n][0] *= a0; oacc[n][1] *= a0;
-                oacc[n][2] *= a1; oacc[n][3] *= a1;
-            }
-        }
-        l0 += ps0;
-        l1 += ps1;
-        // O += P V
-#pragma unroll
-        for (int kk = 0; kk < KPW / 16; ++kk) {
-            const int key = koff + kk * 16 + (mi & 1) * 8 + rin;
-#pragma unroll
-            for (int nbp = 0; nbp < D / 16; ++nbp) {
-                const int ch = 2 * nbp + (mi >> 1);
-                uint32_t v0, v1, v2, v3;
-                ldmatrix_x4_trans(vbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), v0, v1, v2, v3);
-                mma_bf16_16816(oacc[2 * nbp], pa[kk], v0, v1);
-                mma_bf16_16816(oacc[2 * nbp + 1], pa[kk], v2, v3);
-            }
-        }
-    }
-    // The unit's end in this CTA: merge the key slices through this tile's place in the ring; each slice's warp finishes its share of
-    // the columns.  ml [KS][ROWS].
-    template <typename Sync>
-    __device__ __forceinline__ bool finish(const PagedParams& p, const TileDesc& ti, uint8_t* kt, float2* ml, int warp, int slot, Sync&& sync) {
-        const int lane = threadIdx.x & 31, quad = lane >> 2, tq = lane & 3, rg = warp % NW, ks = warp / NW;
-        l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
-        l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-        float tm0 = m0 * p.scale_log2, tm1 = m1 * p.scale_log2;          // log2 domain
-        if (KS > 1) {
-            if (tq == 0) {
-                ml[ks * ROWS + rg * 16 + quad] = make_float2(tm0, l0);
-                ml[ks * ROWS + rg * 16 + quad + 8] = make_float2(tm1, l1);
-            }
-            if (!sync()) return false;
-            float w0[KS], w1[KS];
-            float2 ml0[KS], ml1[KS];
-#pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                ml0[o] = ml[o * ROWS + rg * 16 + quad];
-                ml1[o] = ml[o * ROWS + rg * 16 + quad + 8];
-                tm0 = fmaxf(tm0, ml0[o].x);
-                tm1 = fmaxf(tm1, ml1[o].x);
-            }
-            l0 = l1 = 0.f;
-            const float r0 = tm0 == -INFINITY ? 0.f : tm0, r1 = tm1 == -INFINITY ? 0.f : tm1;
-#pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                w0[o] = fast_exp2(ml0[o].x - r0);
-                w1[o] = fast_exp2(ml1[o].x - r1);
-                l0 += ml0[o].y * w0[o];
-                l1 += ml1[o].y * w1[o];
-            }
-            float4* xch = reinterpret_cast<float4*>(kt);       // [finishing slice][other slices][row group][block of 8 columns][lane]
-#pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                if (o == ks) continue;
-#pragma unroll
-                for (int i = 0; i < NBK; ++i) {
-                    const float (&v)[4] = oacc[o * NBK + i];
-                    xch[(((o * (KS - 1) + (ks < o ? ks : ks - 1)) * NW + rg) * NBK + i) * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
-                }
-            }
-            if (!sync()) return false;
-#pragma unroll
-            for (int o = 0; o < KS; ++o) {
-                if (o != ks) continue;
-#pragma unroll
-                for (int i = 0; i < NBK; ++i) {
-                    float (&v)[4] = oacc[o * NBK + i];
-                    v[0] *= w0[o]; v[1] *= w0[o]; v[2] *= w1[o]; v[3] *= w1[o];
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        if (s == o) continue;
-                        const float4 x = xch[(((o * (KS - 1) + (s < o ? s : s - 1)) * NW + rg) * NBK + i) * 32 + lane];
-                        v[0] += x.x * w0[s]; v[1] += x.y * w0[s];
-                        v[2] += x.z * w1[s]; v[3] += x.w * w1[s];
-                    }
-                }
-            }
-        }
-        const bool whole = ti.n_parts == 1;
-        const float inv0 = whole ? inverse_sum(l0) : 1.f, inv1 = whole ? inverse_sum(l1) : 1.f;
-        const int h0 = ti.kvh * p.g + g0, h1 = ti.kvh * p.g + g1;
-        const size_t orow0 = (static_cast<size_t>(ti.b) * p.L + i0) * p.Hq + h0, orow1 = (static_cast<size_t>(ti.b) * p.L + i1) * p.Hq + h1;
-        float* po = p.part_o + static_cast<size_t>(slot) * ROWS * D;
-#pragma unroll
-        for (int o = 0; o < KS; ++o) {
-            if (o != ks) continue;
-#pragma unroll
-            for (int i = 0; i < NBK; ++i) {
-                const float (&v)[4] = oacc[o * NBK + i];
-                const int col = (o * NBK + i) * 8 + tq * 2;
-                if (whole) {
-                    if (live0) *reinterpret_cast<uint32_t*>(p.out + orow0 * D + col) = pack_bf16(v[0] * inv0, v[1] * inv0);
-                    if (live1) *reinterpret_cast<uint32_t*>(p.out + orow1 * D + col) = pack_bf16(v[2] * inv1, v[3] * inv1);
-                } else {
-                    if (live0) *reinterpret_cast<float2*>(po + (rg * 16 + quad) * D + col) = make_float2(v[0], v[1]);
-                    if (live1) *reinterpret_cast<float2*>(po + (rg * 16 + quad + 8) * D + col) = make_float2(v[2], v[3]);
-                }
-            }
-        }
-        if (ks == 0 && tq == 0) {
-            if (whole) {
-                if (p.lse != nullptr) {
-                    if (live0) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h0) * p.L + i0] = log_sum(tm0, l0);
-                    if (live1) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h1) * p.L + i1] = log_sum(tm1, l1);
-                }
-            } else {
-                float2* pm = reinterpret_cast<float2*>(p.part_ml) + static_cast<size_t>(slot) * ROWS + rg * 16 + quad;
-                pm[0] = make_float2(tm0, l0);
-                pm[8] = make_float2(tm1, l1);
-            }
-        }
-        return true;
-    }
-};
-
-template <int D, int NW, int KS>
-__global__ void __launch_bounds__((PagedShape<D, NW, KS>::WARPS + 1) * 32, 2)
+template <int D>
+__global__ void __launch_bounds__((PG_WARPS + 1) * 32, 2)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
-    using S = PagedShape<D, NW, KS>;
-    constexpr int STAGES = S::STAGES, NCW = S::WARPS;
+    using S = PagedShape<D>;
+    constexpr int STAGES = S::STAGES, NCW = PG_WARPS;
     extern __shared__ uint8_t smem_raw[];
-    const PagedSmem<D, NW, KS> sm(smem_raw);
+    const PagedSmem<D> sm(smem_raw);
     PagedBarriers<STAGES>* bars = sm.bars;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = threadIdx.x >> 5;
@@ -769,17 +526,16 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         prefetch_tensormap(&tm_k);
         prefetch_tensormap(&tm_v);
     }
-    if (S::Q_SMEM) {                             // rows that are no query's: zero, once
-        for (int o = threadIdx.x; o < STAGES * S::Q_STAGE / 16; o += (NCW + 1) * 32) reinterpret_cast<uint4*>(sm.q)[o] = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-    }
+    // rows that are no query's: zero, once
+    for (int o = threadIdx.x; o < STAGES * S::Q_STAGE / 16; o += (NCW + 1) * 32) reinterpret_cast<uint4*>(sm.q)[o] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
     __syncthreads();
     pdl_wait();
 
     if (warp == NCW) {
-        produce<D, NW, KS>(&tm_k, &tm_v, p, sm);
+        produce<D>(&tm_k, &tm_v, p, sm);
     } else {
-        std::conditional_t<S::FEW, FewRows<D, KS>, ManyRows<D, S::FEW ? 1 : NW, KS>> c;
+        FewRows<D> c(p);
         int stage = 0, n_shared = 0;
         uint32_t phase = 0, merge_phase = 0, parity = 0;
         // a barrier among the consumer warps, bounded as all waits are
@@ -790,13 +546,12 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             merge_phase ^= 1;
             return __all_sync(0xffffffffu, ok);
         };
-        c.place(p, warp);
         while (true) {
             if (!__all_sync(0xffffffffu, mbar_wait(&bars->full[stage], phase, abort_flag))) break;
             const TileDesc ti = bars->tile[stage];
             if (ti.flags & TILE_NONE) break;
             uint8_t* kt = sm.tiles + stage * S::STAGE;
-            if (ti.flags & TILE_FIRST) c.first(p, ti, sm.q + stage * S::Q_STAGE, S::Q_ROW, warp);
+            if (ti.flags & TILE_FIRST) c.first(sm.q + stage * S::Q_STAGE);
             c.tile(p, ti, kt, warp);
             const int this_stage = stage;
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -806,7 +561,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 continue;
             }
             const int slot = blockIdx.x * 2 + (static_cast<int>(blockIdx.x) == ti.first_cta ? ti.first_slot : 0);
-            if (!c.finish(p, ti, kt, sm.ml + parity * KS * S::ROWS, warp, slot, merge_sync)) break;
+            if (!c.finish(p, ti, kt, sm.ml + parity * NCW * PG_ROWS, warp, slot, merge_sync)) break;
             parity ^= 1;                                       // (a warp may be a unit ahead of one that still reads its sums)
             fence_proxy_async_smem();                          // (the next copy into this place is the producer's)
             __syncwarp();
@@ -828,7 +583,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 }
                 if (!merge_sync()) break;
                 for (int k = 0; k < 2; ++k)
-                    if ((n_shared >> k & 1) && bars->arrived[k]) join_parts<D, S::ROWS, NCW * 32>(p, bars->shared_unit[k]);
+                    if ((n_shared >> k & 1) && bars->arrived[k]) join_parts<D>(p, bars->shared_unit[k]);
             }
             break;
         }
@@ -844,18 +599,13 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
 }
 
-// Row groups per CTA, by the packed query rows R of a (sequence, KV head): up to 8 rows are the MMA's columns (0), up to 16 its
-// rows, four key slices each; up to 32 two groups of two slices; more take four groups per chunk of 64 rows.
-int paged_row_groups(int R) { return R <= 8 ? 0 : R <= 16 ? 1 : R <= 32 ? 2 : 4; }
-int paged_chunk_rows(int nw) { return nw == 0 ? 8 : nw * 16; }
-
-template <int D, int NW, int KS>
+template <int D>
 int launch_paged(const dare_ctx* ctx, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const PagedParams& p, int ctas, cudaStream_t stream) {
-    using S = PagedShape<D, NW, KS>;
+    using S = PagedShape<D>;
     static_assert(2 * (S::SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
     static std::atomic<uint64_t> smem_set{0};
-    if (ensure_dynamic_smem(smem_set, attn_paged_kernel<D, NW, KS>, S::SMEM) != DARE_OK) return DARE_ERR_CUDA;
-    return launch_kernel(attn_paged_kernel<D, NW, KS>, dim3(ctas), (S::WARPS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
+    if (ensure_dynamic_smem(smem_set, attn_paged_kernel<D>, S::SMEM) != DARE_OK) return DARE_ERR_CUDA;
+    return launch_kernel(attn_paged_kernel<D>, dim3(ctas), (PG_WARPS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -870,32 +620,39 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     if (!ctx || !q || !k_pages || !v_pages || !block_table || !kv_lens || !out) return DARE_ERR_NULL;
     if (int rc = check_current_device(ctx)) return rc;
     if (B < 1 || L < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (d != 64 && d != 128)) return DARE_ERR_SHAPE;
-    if (static_cast<long long>(L) * (Hq / Hkv) > (1 << 20)) return DARE_ERR_SHAPE;
+    if (static_cast<long long>(L) * (Hq / Hkv) > (1 << 20) || Hq / Hkv > 128) return DARE_ERR_SHAPE;
     if (int rc = check_pages(B, max_pages, n_pages, page_size, Hkv)) return rc;
     if (!(scale >= 0.f) || isinf(scale) || window < 0 || sinks < 0) return DARE_ERR_RANGE;
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return DARE_ERR_ALIGN;
+    PagedAttnArgs a;
+    a.B = B; a.L = L; a.Hq = Hq; a.Hkv = Hkv; a.d = d; a.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
+    a.n_pages = n_pages; a.max_pages = max_pages;
+    // a window that reaches further than any key is none (and keeps the kernels' sums within 32 bits)
+    a.window = window >= (max_pages << a.page_shift) ? 0 : window;
+    a.sinks = a.window > 0 ? sinks : 0;
+    a.scale = scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(d));
+    a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.table = block_table; a.kv_lens = kv_lens; a.out = out; a.lse = lse;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // Up to PG_ROWS packed query rows take the kernel of this file, more the tcgen05 kernel.  us here / there: 7 rows, 1 sequence of 8000
+    // keys 16.4 / 16.9, 18 of 2000 19.5 / 21.3, 74 of 1000 29.1 / 32.5.  With the rows as the MMA's 16 rows instead of its 8 columns, 9
+    // to 16 rows took 25.6 / 17.3, 22.4 / 21.3 and 31.4 / 32.7, and 32 rows 46 / 17.5, 38 / 21.6 and 39.5 / 33.4.
+    if (L * (Hq / Hkv) > PG_ROWS) return launch_attn_paged_tc(ctx, a, s);
+
     PagedParams p = {};
     p.B = B; p.L = L; p.Hq = Hq; p.Hkv = Hkv; p.g = Hq / Hkv; p.R = L * p.g;
-    const int nw = paged_row_groups(p.R);
-    const int rows = paged_chunk_rows(nw);
-    p.chunks = (p.R + rows - 1) / rows;
-    p.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
-    p.n_pages = n_pages; p.max_pages = max_pages;
-    // a window that reaches further than any key is none (and keeps the kernel's sums within 32 bits)
-    p.window = window >= (max_pages << p.page_shift) ? 0 : window;
-    p.sinks = p.window > 0 ? sinks : 0;
-    p.scale_log2 = (scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(d))) * LOG2E_F;
+    p.page_shift = a.page_shift; p.n_pages = n_pages; p.max_pages = max_pages; p.window = a.window; p.sinks = a.sinks;
+    p.scale_log2 = a.scale * LOG2E_F;
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.table = block_table; p.kv_lens = kv_lens;
     p.out = static_cast<__nv_bfloat16*>(out); p.lse = lse;
     p.counters = ctx->join_counters; p.dev_status = ctx->dev_status;
     // two CTAs per SM, all resident at once; no more than there can be tiles
-    const long long tiles = static_cast<long long>(B) * Hkv * p.chunks * ((static_cast<long long>(max_pages) * page_size + PG_KT - 1) / PG_KT);
+    const long long tiles = static_cast<long long>(B) * Hkv * ((static_cast<long long>(max_pages) * page_size + PG_KT - 1) / PG_KT);
     if (tiles > (1LL << 30)) return DARE_ERR_SHAPE;
     long long ctas = 2LL * ctx->sm_count;
     if (ctas > PAGED_MAX_CTAS) ctas = PAGED_MAX_CTAS;
     if (ctas > tiles) ctas = tiles;
-    const size_t part_rows = static_cast<size_t>(ctas) * 2 * rows;
+    const size_t part_rows = static_cast<size_t>(ctas) * 2 * PG_ROWS;
     if (part_rows * (d + 2) * sizeof(float) > ctx->workspace_bytes) return DARE_ERR_WORKSPACE;
     p.part_o = static_cast<float*>(ctx->workspace);
     p.part_ml = p.part_o + part_rows * d;
@@ -905,11 +662,6 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     int rc = make_tmap_bf16_2d(ctx, &tm_k, k_pages, pool_rows, d, box_rows, 64);
     if (rc == DARE_OK) rc = make_tmap_bf16_2d(ctx, &tm_v, v_pages, pool_rows, d, box_rows, 64);
     if (rc != DARE_OK) return rc;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int n = static_cast<int>(ctas);
-    if (d == 128)
-        return nw == 0 ? launch_paged<128, 0, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 1 ? launch_paged<128, 1, 4>(ctx, tm_k, tm_v, p, n, s)
-             : nw == 2 ? launch_paged<128, 2, 2>(ctx, tm_k, tm_v, p, n, s) : launch_paged<128, 4, 1>(ctx, tm_k, tm_v, p, n, s);
-    return nw == 0 ? launch_paged<64, 0, 4>(ctx, tm_k, tm_v, p, n, s) : nw == 1 ? launch_paged<64, 1, 4>(ctx, tm_k, tm_v, p, n, s)
-         : nw == 2 ? launch_paged<64, 2, 2>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64, 4, 1>(ctx, tm_k, tm_v, p, n, s);
+    return d == 128 ? launch_paged<128>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64>(ctx, tm_k, tm_v, p, n, s);
 }

@@ -238,7 +238,7 @@ def _check_attend(out, lse, q, kp, vp, table, lens, window, sinks, scale=0.0):
         gl = lse.cpu().double().numpy()
         assert (np.isneginf(gl) == np.isneginf(rl)).all()
         fin = np.isfinite(rl)
-        assert (np.abs(gl - rl)[fin] <= (s + 2.0 ** -16 * (1 + np.abs(rl) + sabs))[fin]).all()
+        assert (np.abs(gl[fin] - rl[fin]) <= (s + 2.0 ** -16 * (1 + np.abs(rl) + sabs))[fin]).all()
 
 
 def _attend(ctx, q, kp, vp, table, lens, window, sinks, lse=True, **kw):
@@ -292,6 +292,44 @@ def test_attend(ctx, L, hq, hkv, d, page, lens, window, sinks):
     _check_attend(out, lse, q, kp, vp, table, lens, window, sinks)
     again, lse2 = _attend(ctx, q, kp, vp, table, lens, window, sinks)
     assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("L,hq,hkv,d,page,n_seqs,longest,window,sinks", [
+    (32, 28, 4, 128, 64, 7, 300, 0, 0),                      # 224 rows in two tiles, one of them half full
+    (32, 28, 4, 128, 16, 29, 150, 0, 0),                     # both tiles of a pair
+    (32, 28, 4, 128, 32, 29, 260, 50, 3),
+    (32, 28, 4, 128, 16, 7, 700, 64, 70),
+    (97, 4, 4, 64, 16, 10, 300, 0, 0),                       # one tile per sequence, 31 rows of it empty
+    (130, 16, 4, 64, 128, 13, 260, 0, 0),                    # five tiles
+    (130, 16, 4, 64, 32, 13, 330, 33, 4),
+    (200, 2, 2, 128, 16, 10, 420, 1, 0),
+    (40, 3, 1, 128, 1024, 40, 130, 0, 0),                    # 120 rows: 42 positions of 3 heads
+])
+def test_attend_many_rows(ctx, L, hq, hkv, d, page, n_seqs, longest, window, sinks):
+    """Enough units of 96 rows and more for the tcgen05 kernel."""
+    rng = np.random.default_rng(L + n_seqs)
+    lens = [0 if i % 11 == 5 else int(n) for i, n in enumerate(rng.integers(L, longest, n_seqs))]
+    lens[0], lens[1], lens[-1] = longest, L, -(-L // 64) * 64
+    q, kp, vp, table = _attend_case(L, n_seqs, L, hq, hkv, d, page, lens, window, sinks)
+    out, lse = _attend(ctx, q, kp, vp, table, lens, window, sinks)
+    assert ctx.device_status() == 0
+    _check_attend(out, lse, q, kp, vp, table, lens, window, sinks)
+    again, lse2 = _attend(ctx, q, kp, vp, table, lens, window, sinks)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+def test_attend_many_rows_reports_lengths_and_pages_outside(ctx):
+    lens = [100, 128, 40, 60, 70, 80, 90, 100, 110, 120]
+    q, kp, vp, table = _attend_case(3, 10, 32, 28, 4, 64, 16, lens, 0, 0, plant=False)
+    given = [table.shape[1] * 16 + 5, -3] + lens[2:]
+    table[0, 7] = table[1, 7]
+    out, lse = _attend(ctx, q, kp, vp, table, given, 0, 0)
+    assert ctx.device_status() == dare.DEV_LEN_CLAMPED
+    _check_attend(out, lse, q, kp, vp, table, [table.shape[1] * 16, 0] + lens[2:], 0, 0)
+    table[3, 1], table[4, 0] = -1, kp.shape[0]
+    out, lse = _attend(ctx, q, kp, vp, table, lens, 0, 0)
+    assert ctx.device_status() == dare.DEV_INDEX_OUTSIDE
+    _check_attend(out, lse, q, kp, vp, table, lens, 0, 0)
 
 
 @pytest.mark.parametrize("L", [1, 3, 40])
@@ -509,6 +547,7 @@ def test_refusals(ctx):
     assert attend(q=(2, 1, 4, 32), pool=(5, 2, 16, 32)) == -2 and attend(q=(2, 1, 5, 64)) == -2
     for empty in (dict(q=(0, 1, 4, 64), table=(0, 3)), dict(q=(2, 0, 4, 64)), dict(table=(2, 0)), dict(pool=(0, 2, 16, 64))):
         assert attend(**empty) == -1                         # (an empty tensor has no address)
+    assert attend(q=(2, 1, 258, 64)) == -2                   # 129 query heads per KV head
     assert attend(window=-1) == -4 and attend(sinks=-1) == -4 and attend(scale=-1.0) == -4 and attend(scale=float("nan")) == -4
     assert attend(scale=float("inf")) == -4
     rope = torch.zeros(10, 32, 2, device="cuda")
