@@ -6,9 +6,12 @@
 //     r = 1 / sqrt(mean(x^2) + eps),  y = x r w,  (o_c, o_{c+d/2}) = (y_c cos - y_{c+d/2} sin, y_{c+d/2} cos + y_c sin)
 // fp32 inside, rounded to bf16 once, at the end.  Its gradient, with g the output's: z = g turned back by the same angle,
 //     dw += z x r,   dx = r (w z - x r mean(w z x r)).
-// Everything here is one pass over memory.  A head is held by d / 16 lanes, 8 channels c.. and their partners c + d/2.. each
-// (two 16-byte pieces), so that a norm is three (two) shuffles and a rotation none; a warp takes a row, or a part of its
-// heads where rows are few, keeps the row's 8 angles and the weights in registers and walks the heads.
+// Everything here is one pass over memory and bound by it, and next to it by the instructions that unpack, add up, rotate and pack.
+// The work is cut into items, runs of heads that lie side by side in a row (whole rows, where they fit a stage and there are enough
+// of them); a warp takes every so many of them through a ring of its own: bulk copies bring the next item to shared memory while
+// the warp works on this one in place, and bulk copies take it away.  So what is in flight does not hang on registers.
+// A head is held by d / 16 lanes, 8 channels c.. and their partners c + d/2.. each (two 16-byte pieces), so that a norm is three
+// (two) shuffles and a rotation none; the weights are multiplied into the angles once per item.
 #include <math.h>
 
 #include "internal.h"
@@ -17,49 +20,83 @@
 namespace dare {
 namespace {
 
-constexpr int QKN_WARPS = 8;        // warps per CTA
+enum { QKN_DENSE = 0, QKN_APPEND = 1, QKN_BACKWARD = 2 };
+
+// One CTA per SM.  Stage: of an item's run of heads, in the backward pass of values and of gradients.  us at 19201 rows of 28 + 4 + 4
+// heads of 128, forward / backward, for 12 warps x 2 stages of 9216 bytes 67.9 / 89.5, 16 x 3 of 4608 57.6 / 151.5 (128 registers: spills), 12 x 3
+// of 6144 67.4 / 90.8, 16 x 2 of 6144 68.9 / 112.9, 8 x 3 of 9216 64.9 / 96.1, 24 x 2 of 4608 116 / 211.
+template <int MODE>
+struct QkNormShape {
+    static constexpr int WARPS = MODE == QKN_BACKWARD ? 12 : 16;             // at most
+    static constexpr int STAGES = MODE == QKN_BACKWARD ? 2 : 3;
+    static constexpr int STAGE_BYTES = MODE == QKN_BACKWARD ? 9216 : 4608;
+};
 
 struct QkNormParams {
-    const uint4* qkv;               // [rows, (Hq + 2 Hkv) d]
+    const __nv_bfloat16* qkv;                      // [rows, (Hq + 2 Hkv) d]
     int rows, Hq, Hkv;
-    const uint4 *wq, *wk;           // bf16 [d], or NULL: no norm
+    const uint4 *wq, *wk;                          // bf16 [d], or NULL: no norm
     float eps;
-    const int32_t* positions;       // [rows]
-    const float4* rope;             // [n_positions, d/2] (cos, sin)
+    const int32_t* positions;                      // [rows]
+    const float4* rope;                            // [n_positions, d/2] (cos, sin)
     int n_positions;
-    int warps_per_row;
-    uint4 *q_out, *k_out, *v_out;   // [rows, Hq, d], [rows, Hkv, d] (append: k_out and v_out are the pages)
+    int item_heads, row_items;                     // heads of an item, items of a row
+    __nv_bfloat16 *q_out, *k_out, *v_out;          // [rows, Hq, d], [rows, Hkv, d] (append: k_out and v_out are the pages)
     // append
     const int32_t *seq_ids, *table;
     int n_seqs, max_pages, n_pages, page_shift;
+    // backward
+    const __nv_bfloat16 *gq, *gk, *gv;             // [rows, Hq, d], [rows, Hkv, d] twice
+    __nv_bfloat16* dx;                             // [rows, (Hq + 2 Hkv) d]
+    float* part;                                   // [CTAs][2][d] sums of the weights' gradients
     uint32_t* dev_status;
 };
 
-struct QkNormGradParams {
-    const uint4* qkv;
-    int rows, Hq, Hkv;
-    const uint4 *wq, *wk;
-    float eps;
-    const int32_t* positions;
-    const float4* rope;
-    int n_positions;
-    int warps_per_row;
-    const uint4 *gq, *gk, *gv;      // [rows, Hq, d], [rows, Hkv, d] twice
-    uint4* dx;                      // [rows, (Hq + 2 Hkv) d]
-    float* part;                    // [CTAs][2][d] sums of the weights' gradients
-    uint32_t* dev_status;
+// An item: heads [h0, h0 + nq + nk + nv) of a row: nq query heads from q0 on, nk key heads from k0 on, nv value heads from v0 on.
+struct Item {
+    int row, h0, nq, nk, nv, q0, k0, v0;
+    __device__ __forceinline__ Item(int row_, int k, int per, int Hq, int Hkv) : row(row_), h0(k * per) {
+        const int end = min(h0 + per, Hq + 2 * Hkv);
+        q0 = min(h0, Hq);
+        nq = min(end, Hq) - q0;
+        k0 = min(max(h0 - Hq, 0), Hkv);
+        nk = min(max(end - Hq, 0), Hkv) - k0;
+        v0 = max(h0 - Hq - Hkv, 0);
+        nv = max(end - Hq - Hkv, 0) - v0;
+    }
+};
+// The place of an item in the list of all rows' items, walked in steps of one size.
+struct ItemWalk {
+    int row, k, n, row_step, k_step;
+    __device__ __forceinline__ ItemWalk(int first, int step, int n_)
+        : row(first / n_), k(first - row * n_), n(n_), row_step(step / n_), k_step(step - row_step * n_) {}
+    __device__ __forceinline__ void next() {
+        row += row_step;
+        k += k_step;
+        if (k >= n) { k -= n; ++row; }
+    }
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+// Eight bf16 values as four pairs of fp32, and back.
+__device__ __forceinline__ void unpack8(const uint4& v, uint64_t (&f)[4]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) f[i] = pack_b32x2(w[i] << 16, w[i] & 0xffff0000u);
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+__device__ __forceinline__ uint4 pack8(const uint64_t (&f)[4]) {
+    return make_uint4(pack_bf16(lo_f32x2(f[0]), hi_f32x2(f[0])), pack_bf16(lo_f32x2(f[1]), hi_f32x2(f[1])),
+                      pack_bf16(lo_f32x2(f[2]), hi_f32x2(f[2])), pack_bf16(lo_f32x2(f[3]), hi_f32x2(f[3])));
+}
+__device__ __forceinline__ uint64_t both(float x) { return pack_f32x2(x, x); }
+__device__ __forceinline__ float dot8(const uint64_t (&a)[4], const uint64_t (&b)[4], const uint64_t (&c)[4], const uint64_t (&d)[4]) {
+    uint64_t s = mul_f32x2(a[0], b[0]), t = mul_f32x2(c[0], d[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) {
+        s = fma_f32x2(a[j], b[j], s);
+        t = fma_f32x2(c[j], d[j], t);
+    }
+    s = add_f32x2(s, t);
+    return lo_f32x2(s) + hi_f32x2(s);
 }
 template <int LANES>
 __device__ __forceinline__ float sum_lanes(float x) {
@@ -68,213 +105,299 @@ __device__ __forceinline__ float sum_lanes(float x) {
     return x;
 }
 
-// The 8 angles of a lane's channels at position pos (two to a 16-byte load).
+// The forward pass of `heads` heads of one kind, in place: o = r (a (wa cos) - b (wb sin)), r (b (wb cos) + a (wa sin)).
 template <int D>
-__device__ __forceinline__ void load_angles(const float4* rope, int64_t pos, int piece, bool inside, float (&cs)[8], float (&sn)[8]) {
+__device__ __forceinline__ void rotate_heads(uint8_t* at, int heads, const uint4* w, float eps, const uint64_t (&cs)[4], const uint64_t (&sn)[4]) {
+    constexpr int LANES = D / 16, PER = 32 / LANES;
+    const int lane = threadIdx.x & 31, piece = lane % LANES, sub = lane / LANES;
+    uint64_t ca[4], sb[4], cb[4], sa[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float4 t = inside ? rope[pos * (D / 4) + piece * 4 + j] : make_float4(0.f, 0.f, 0.f, 0.f);
-        cs[2 * j] = t.x;
-        sn[2 * j] = t.y;
-        cs[2 * j + 1] = t.z;
-        sn[2 * j + 1] = t.w;
+        ca[j] = cb[j] = cs[j];
+        sa[j] = sn[j];
+        sb[j] = sn[j] ^ 0x8000000080000000ull;
+    }
+    if (w != nullptr) {
+        uint64_t wa[4], wb[4];
+        unpack8(w[piece], wa);
+        unpack8(w[LANES + piece], wb);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ca[j] = mul_f32x2(ca[j], wa[j]);
+            sa[j] = mul_f32x2(sa[j], wa[j]);
+            cb[j] = mul_f32x2(cb[j], wb[j]);
+            sb[j] = mul_f32x2(sb[j], wb[j]);
+        }
+    }
+    uint4* x = reinterpret_cast<uint4*>(at + sub * D * 2) + piece;
+#pragma unroll 2
+    for (int h = 0; h < heads; h += PER, x += PER * D / 8) {
+        const bool live = h + sub < heads;         // (beyond the last head lies whatever the stage holds: not written)
+        uint64_t a[4], b[4], lo[4], hi[4];
+        unpack8(x[0], a);
+        unpack8(x[LANES], b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = fma_f32x2(a[j], ca[j], mul_f32x2(b[j], sb[j]));
+            hi[j] = fma_f32x2(b[j], cb[j], mul_f32x2(a[j], sa[j]));
+        }
+        if (w != nullptr) {
+            const uint64_t r = both(rsqrtf(sum_lanes<LANES>(dot8(a, a, b, b)) * (1.f / D) + eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = mul_f32x2(lo[j], r);
+                hi[j] = mul_f32x2(hi[j], r);
+            }
+        }
+        if (live) {
+            x[0] = pack8(lo);
+            x[LANES] = pack8(hi);
+        }
     }
 }
 
-// A row's heads in groups of 32 / LANES, queries, keys and values each starting a group of its own (so that a group's kind is
-// the same in all lanes).
-struct HeadGroups {
-    int nq, nk, n;       // groups of queries, of keys (and as many of values), of all
-    __device__ __forceinline__ HeadGroups(int Hq, int Hkv, int per) : nq((Hq + per - 1) / per), nk((Hkv + per - 1) / per), n(nq + 2 * nk) {}
-};
-
-// Where a lane's head of group `grp` is: kind 0 q, 1 k, 2 v; h the head within its kind; live: there is such a head.
-struct HeadPlace {
-    int kind, h, count;
-    bool live;
-    __device__ __forceinline__ HeadPlace(const HeadGroups& hg, int grp, int sub, int per, int Hq, int Hkv) {
-        kind = grp < hg.nq ? 0 : grp < hg.nq + hg.nk ? 1 : 2;
-        h = (grp - (kind == 0 ? 0 : kind == 1 ? hg.nq : hg.nq + hg.nk)) * per + sub;
-        count = kind == 0 ? Hq : Hkv;
-        live = h < count;
-    }
-};
-
-template <int D, bool APPEND>
-__global__ void __launch_bounds__(QKN_WARPS * 32)
-qk_norm_rope_kernel(const QkNormParams p) {
-    constexpr int LANES = D / 16, PER = 32 / LANES, V8 = D / 8;      // lanes per head, heads per warp, 16-byte pieces per head
+// The backward pass of `heads` heads of one kind: gradients g in place, the heads' values x; acc: the weight's gradient so far.
+template <int D>
+__device__ __forceinline__ void rotate_heads_back(uint8_t* g_at, const uint8_t* x_at, int heads, const uint4* w, float eps, const uint64_t (&cs)[4],
+                                                  const uint64_t (&sn)[4], uint64_t (&acc)[8]) {
+    constexpr int LANES = D / 16, PER = 32 / LANES;
     const int lane = threadIdx.x & 31, piece = lane % LANES, sub = lane / LANES;
-    const int item = blockIdx.x * QKN_WARPS + (threadIdx.x >> 5);
-    const int row = item / p.warps_per_row, part = item % p.warps_per_row;
+    uint64_t wa[4], wb[4], ns[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ns[j] = sn[j] ^ 0x8000000080000000ull;
+    if (w != nullptr) {
+        unpack8(w[piece], wa);
+        unpack8(w[LANES + piece], wb);
+    }
+    uint4* g = reinterpret_cast<uint4*>(g_at + sub * D * 2) + piece;
+    const uint4* x = reinterpret_cast<const uint4*>(x_at + sub * D * 2) + piece;
+    for (int h = 0; h < heads; h += PER, g += PER * D / 8, x += PER * D / 8) {
+        const bool live = h + sub < heads;
+        uint64_t ga[4], gb[4], za[4], zb[4];
+        unpack8(g[0], ga);
+        unpack8(g[LANES], gb);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            za[j] = fma_f32x2(ga[j], cs[j], mul_f32x2(gb[j], sn[j]));
+            zb[j] = fma_f32x2(gb[j], cs[j], mul_f32x2(ga[j], ns[j]));
+        }
+        if (w != nullptr) {
+            uint64_t xa[4], xb[4], ya[4], yb[4];
+            unpack8(x[0], xa);
+            unpack8(x[LANES], xb);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                ya[j] = mul_f32x2(wa[j], za[j]);
+                yb[j] = mul_f32x2(wb[j], zb[j]);
+            }
+            const float r = rsqrtf(sum_lanes<LANES>(dot8(xa, xa, xb, xb)) * (1.f / D) + eps);
+            const float m = sum_lanes<LANES>(dot8(ya, xa, yb, xb)) * r * (1.f / D);            // mean(w z x r)
+            const uint64_t rr = both(r), mr = both(-m * r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                xa[j] = mul_f32x2(xa[j], rr);                                // x r
+                xb[j] = mul_f32x2(xb[j], rr);
+                if (live) {
+                    acc[j] = fma_f32x2(za[j], xa[j], acc[j]);
+                    acc[4 + j] = fma_f32x2(zb[j], xb[j], acc[4 + j]);
+                }
+                za[j] = fma_f32x2(xa[j], mr, mul_f32x2(ya[j], rr));
+                zb[j] = fma_f32x2(xb[j], mr, mul_f32x2(yb[j], rr));
+            }
+        }
+        if (live) {
+            g[0] = pack8(za);
+            g[LANES] = pack8(zb);
+        }
+    }
+}
+
+template <int D, int MODE>
+__global__ void __launch_bounds__(QkNormShape<MODE>::WARPS * 32, 1)
+qk_norm_kernel(const QkNormParams p) {
+    constexpr int QKN_WARPS = QkNormShape<MODE>::WARPS, QKN_STAGES = QkNormShape<MODE>::STAGES, QKN_STAGE_BYTES = QkNormShape<MODE>::STAGE_BYTES;
+    constexpr bool BACK = MODE == QKN_BACKWARD, APPEND = MODE == QKN_APPEND;
+    constexpr int LANES = D / 16, HEAD = D * 2;                              // lanes per head, bytes
+    constexpr int SECOND = BACK ? QKN_STAGE_BYTES / 2 : 0;                   // the gradients' half of a stage
+    extern __shared__ __align__(128) uint8_t qkn_smem[];
+    __shared__ uint64_t bars[QKN_WARPS][QKN_STAGES];
+    __shared__ uint4 weights[2][D / 8];                                      // (beside the rings there is little L1 left)
+    __shared__ uint32_t abort_word;
+    volatile uint32_t* abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LANES, sub = lane / LANES, warps = blockDim.x >> 5;
+    uint8_t* ring = qkn_smem + warp * QKN_STAGES * QKN_STAGE_BYTES;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < warps * QKN_STAGES; ++i) mbar_init(&bars[0][0] + i, 1);
+        abort_word = 0;
+        fence_barrier_init();
+    }
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
-    if (row >= p.rows) return;
-    const int pos = p.positions[row];
-    bool inside = pos >= 0 && pos < p.n_positions;
-    int64_t page = 0;
-    if (APPEND) {
-        const int seq = p.seq_ids[row];
-        if (seq < 0) return;                                         // the row belongs to no sequence
-        inside = inside && seq < p.n_seqs && (pos >> p.page_shift) < p.max_pages;
-        if (inside) {
-            page = p.table[static_cast<int64_t>(seq) * p.max_pages + (pos >> p.page_shift)];
-            inside = page >= 0 && page < p.n_pages;
-        }
+    const int heads_in = p.Hq + 2 * p.Hkv;
+    const int step = static_cast<int>(gridDim.x) * warps;
+    const int first = warp * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);      // (few items: spread over the SMs)
+    ItemWalk now(first, step, p.row_items), ahead = now;
+    const bool normed = p.wq != nullptr;
+    if (normed) {
+        for (int c = threadIdx.x; c < 2 * (D / 8); c += blockDim.x) weights[c / (D / 8)][c % (D / 8)] = c < D / 8 ? p.wq[c] : p.wk[c - D / 8];
+        __syncthreads();
     }
-    if (!inside) {
-        if (lane == 0 && part == 0) atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
-        if (APPEND) return;
-    }
-    float cs[8], sn[8];
-    load_angles<D>(p.rope, pos, piece, inside, cs, sn);
-    const HeadGroups hg(p.Hq, p.Hkv, PER);
-    const uint4* src = p.qkv + static_cast<int64_t>(row) * (p.Hq + 2 * p.Hkv) * V8;
-    for (int grp = part; grp < hg.n; grp += p.warps_per_row) {
-        const HeadPlace at(hg, grp, sub, PER, p.Hq, p.Hkv);
-        const int h_in = at.h + (at.kind == 0 ? 0 : at.kind == 1 ? p.Hq : p.Hq + p.Hkv);
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-        if (at.live) {
-            lo = src[h_in * V8 + piece];
-            hi = src[h_in * V8 + LANES + piece];
+    const uint4 *wq = normed ? weights[0] : nullptr, *wk = normed ? weights[1] : nullptr;
+
+    auto send_for = [&](const ItemWalk& w, int stage) {                      // lane 0
+        const Item it(w.row, w.k, p.item_heads, p.Hq, p.Hkv);
+        uint8_t* dst = ring + stage * QKN_STAGE_BYTES;
+        uint64_t* bar = &bars[warp][stage];
+        const uint32_t all = static_cast<uint32_t>(it.nq + it.nk + it.nv) * HEAD;
+        // (the backward pass reads the values of queries and keys, where they are normalised)
+        const uint32_t values = !BACK ? all : normed ? static_cast<uint32_t>(it.nq + it.nk) * HEAD : 0;
+        mbar_arrive_expect_tx(bar, values + (BACK ? all : 0));
+        if (values) bulk_load(dst, p.qkv + (static_cast<int64_t>(it.row) * heads_in + it.h0) * D, values, bar);
+        if (BACK) {
+            dst += SECOND;
+            if (it.nq) bulk_load(dst, p.gq + (static_cast<int64_t>(it.row) * p.Hq + it.q0) * D, it.nq * HEAD, bar);
+            if (it.nk) bulk_load(dst + it.nq * HEAD, p.gk + (static_cast<int64_t>(it.row) * p.Hkv + it.k0) * D, it.nk * HEAD, bar);
+            if (it.nv) bulk_load(dst + (it.nq + it.nk) * HEAD, p.gv + (static_cast<int64_t>(it.row) * p.Hkv + it.v0) * D, it.nv * HEAD, bar);
         }
-        if (at.kind < 2) {
-            float a[8], b[8];
-            unpack8(lo, a);
-            unpack8(hi, b);
-            const uint4* w = at.kind == 0 ? p.wq : p.wk;
-            if (w != nullptr) {
-                float ss = 0.f;
+    };
+
+    uint64_t acc[2][8];                                                      // the weights' gradients, pairs of channels
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss += a[j] * a[j] + b[j] * b[j];
-                const float r = rsqrtf(sum_lanes<LANES>(ss) * (1.f / D) + p.eps);
-                float wa[8], wb[8];
-                unpack8(w[piece], wa);
-                unpack8(w[LANES + piece], wb);
+    for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = 0;
+    for (int s = 0; s < QKN_STAGES - 1; ++s) {
+        if (lane == 0 && ahead.row < p.rows) send_for(ahead, s);
+        ahead.next();
+    }
+    // What an item needs besides its heads is asked for ahead of it, so that nothing waits for it: its position (and sequence) two
+    // items before, its angles (and page) one item before.  (In the backward pass the angles that wait would spill: 106 us instead of 95 at
+    // 19201 rows of 28 + 4 + 4 heads of 128.)
+    struct Place { int pos, seq; };
+    auto place_of = [&](const ItemWalk& w) -> Place {
+        return w.row < p.rows ? Place{p.positions[w.row], APPEND ? p.seq_ids[w.row] : 0} : Place{-1, -1};
+    };
+    struct Angles { float4 t[4]; int page; bool inside; };
+    auto angles_of = [&](const Place& at) -> Angles {
+        Angles a = {};
+        a.inside = at.pos >= 0 && at.pos < p.n_positions;
+        if (APPEND) {
+            a.inside = a.inside && at.seq >= 0 && at.seq < p.n_seqs && (at.pos >> p.page_shift) < p.max_pages;
+            if (a.inside) a.page = p.table[static_cast<int64_t>(at.seq) * p.max_pages + (at.pos >> p.page_shift)];
+        }
+        if (a.inside) {
+            const float4* t = p.rope + static_cast<int64_t>(at.pos) * (D / 4) + piece * 4;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    a[j] *= r * wa[j];
-                    b[j] *= r * wb[j];
+            for (int j = 0; j < 4; ++j) a.t[j] = t[j];
+        }
+        return a;
+    };
+    Place place = place_of(now);
+    ItemWalk later = now;
+    later.next();
+    Place place1 = place_of(later);
+    Angles angles = {};
+    if (!BACK) angles = angles_of(place);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    while (now.row < p.rows) {
+        const Item it(now.row, now.k, p.item_heads, p.Hq, p.Hkv);
+        const bool reports = now.k == 0 && lane == 0;
+        now.next();
+        later.next();
+        const Place place2 = place_of(later);
+        Angles angles1 = {};
+        if (BACK) angles = angles_of(place);
+        else angles1 = angles_of(place1);
+        // the next item takes the last one's place, once its copies out have read it
+        bulk_wait_read();
+        __syncwarp();
+        if (lane == 0 && ahead.row < p.rows) send_for(ahead, stage == 0 ? QKN_STAGES - 1 : stage - 1);
+        ahead.next();
+        uint64_t cs[4], sn[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            cs[j] = pack_f32x2(angles.t[j].x, angles.t[j].z);
+            sn[j] = pack_f32x2(angles.t[j].y, angles.t[j].w);
+        }
+        const int pos = place.pos;
+        const int64_t page = angles.page;
+        const bool inside = angles.inside && (!APPEND || (page >= 0 && page < p.n_pages));
+        if (!inside && reports && !(APPEND && place.seq < 0)) atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
+        ok = __all_sync(0xffffffffu, mbar_wait(&bars[warp][stage], phase, abort_flag));
+        if (!ok) break;
+        uint8_t* at = ring + stage * QKN_STAGE_BYTES + SECOND;               // what is worked on, in place
+        if (!inside) {
+            if (!APPEND)                                                     // (append: the row is left out)
+                for (int o = lane; o < (it.nq + it.nk + it.nv) * (D / 8); o += 32) reinterpret_cast<uint4*>(at)[o] = make_uint4(0, 0, 0, 0);
+        } else if (!BACK) {
+            if (it.nq) rotate_heads<D>(at, it.nq, wq, p.eps, cs, sn);
+            if (it.nk) rotate_heads<D>(at + it.nq * HEAD, it.nk, wk, p.eps, cs, sn);
+        } else {
+            if (it.nq) rotate_heads_back<D>(at, at - SECOND, it.nq, wq, p.eps, cs, sn, acc[0]);
+            if (it.nk) rotate_heads_back<D>(at + it.nq * HEAD, at - SECOND + it.nq * HEAD, it.nk, wk, p.eps, cs, sn, acc[1]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (BACK) {
+            if (lane == 0) bulk_store(p.dx + (static_cast<int64_t>(it.row) * heads_in + it.h0) * D, at, static_cast<uint32_t>(it.nq + it.nk + it.nv) * HEAD);
+        } else if (!APPEND || inside) {
+            if (lane == 0 && it.nq) bulk_store(p.q_out + (static_cast<int64_t>(it.row) * p.Hq + it.q0) * D, at, it.nq * HEAD);
+            at += it.nq * HEAD;
+            if (APPEND) {
+                // A head's place is a row of its page: short for bulk copies (one each cost 37.8 us instead of 36.8 at 7473 rows of 32 + 32 + 32 heads
+                // of 128).
+                const int64_t in_page = pos & ((1 << p.page_shift) - 1);
+                for (int o = lane; o < (it.nk + it.nv) * (D / 8); o += 32) {
+                    const int h = o / (D / 8);
+                    const int64_t head = h < it.nk ? it.k0 + h : it.v0 + h - it.nk;
+                    reinterpret_cast<uint4*>((h < it.nk ? p.k_out : p.v_out) + (((page * p.Hkv + head) << p.page_shift) + in_page) * D)[o % (D / 8)] =
+                        reinterpret_cast<const uint4*>(at)[o];
                 }
+            } else if (lane == 0) {
+                if (it.nk) bulk_store(p.k_out + (static_cast<int64_t>(it.row) * p.Hkv + it.k0) * D, at, it.nk * HEAD);
+                if (it.nv) bulk_store(p.v_out + (static_cast<int64_t>(it.row) * p.Hkv + it.v0) * D, at + it.nk * HEAD, it.nv * HEAD);
             }
-            float x[8], y[8];
+        }
+        bulk_commit();
+        place = place1;
+        place1 = place2;
+        if (!BACK) angles = angles1;
+        if (++stage == QKN_STAGES) { stage = 0; phase ^= 1; }
+    }
+    bulk_wait();
+    if (BACK && normed) {
+        // the CTA's sums, in a fixed order: lanes of the same channels, then the warps
+        __syncthreads();                                                     // (the rings are idle)
+        float* sums = reinterpret_cast<float*>(qkn_smem);                    // [warp][2][D]
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[j] = a[j] * cs[j] - b[j] * sn[j];
-                y[j] = b[j] * cs[j] + a[j] * sn[j];
-            }
-            lo = pack8(x);
-            hi = pack8(y);
-        }
-        if (!at.live) continue;
-        if (!APPEND && !inside) lo = hi = make_uint4(0, 0, 0, 0);
-        uint4* dst;
-        if (at.kind == 0) dst = p.q_out + (static_cast<int64_t>(row) * p.Hq + at.h) * V8;
-        else if (APPEND) dst = (at.kind == 1 ? p.k_out : p.v_out) + (((page * p.Hkv + at.h) << p.page_shift) + (pos & ((1 << p.page_shift) - 1))) * V8;
-        else dst = (at.kind == 1 ? p.k_out : p.v_out) + (static_cast<int64_t>(row) * p.Hkv + at.h) * V8;
-        dst[piece] = lo;
-        dst[LANES + piece] = hi;
-    }
-}
-
-template <int D>
-__global__ void __launch_bounds__(QKN_WARPS * 32)
-qk_norm_rope_backward_kernel(const QkNormGradParams p) {
-    constexpr int LANES = D / 16, PER = 32 / LANES, V8 = D / 8;
-    __shared__ float s_dw[QKN_WARPS][D];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LANES, sub = lane / LANES;
-    float acc[2][16];
+                float x = lo_f32x2(acc[k][j]), y = hi_f32x2(acc[k][j]);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) acc[0][j] = acc[1][j] = 0.f;
-    const HeadGroups hg(p.Hq, p.Hkv, PER);
-    pdl_wait();
-    pdl_trigger();
-    const int64_t items = static_cast<int64_t>(p.rows) * p.warps_per_row;
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * QKN_WARPS + warp; item < items; item += static_cast<int64_t>(gridDim.x) * QKN_WARPS) {
-        const int row = static_cast<int>(item / p.warps_per_row), part = static_cast<int>(item % p.warps_per_row);
-        const int pos = p.positions[row];
-        const bool inside = pos >= 0 && pos < p.n_positions;
-        if (!inside && lane == 0 && part == 0) atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
-        float cs[8], sn[8];
-        load_angles<D>(p.rope, pos, piece, inside, cs, sn);
-        const int64_t row_at = static_cast<int64_t>(row) * (p.Hq + 2 * p.Hkv);
-        for (int grp = part; grp < hg.n; grp += p.warps_per_row) {
-            const HeadPlace at(hg, grp, sub, PER, p.Hq, p.Hkv);
-            const int h_in = at.h + (at.kind == 0 ? 0 : at.kind == 1 ? p.Hq : p.Hq + p.Hkv);
-            const uint4* g = (at.kind == 0 ? p.gq : at.kind == 1 ? p.gk : p.gv) + (static_cast<int64_t>(row) * at.count + at.h) * V8;
-            uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-            const bool on = at.live && inside;
-            if (on) {
-                lo = g[piece];
-                hi = g[LANES + piece];
-            }
-            if (at.kind < 2) {
-                float ga[8], gb[8], za[8], zb[8];
-                unpack8(lo, ga);
-                unpack8(hi, gb);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    za[j] = ga[j] * cs[j] + gb[j] * sn[j];
-                    zb[j] = gb[j] * cs[j] - ga[j] * sn[j];
+                for (int off = LANES; off < 32; off <<= 1) {
+                    x += __shfl_xor_sync(0xffffffffu, x, off);
+                    y += __shfl_xor_sync(0xffffffffu, y, off);
                 }
-                const uint4* w = at.kind == 0 ? p.wq : p.wk;
-                if (w != nullptr) {
-                    uint4 xlo = make_uint4(0, 0, 0, 0), xhi = xlo;
-                    if (on) {
-                        xlo = p.qkv[(row_at + h_in) * V8 + piece];
-                        xhi = p.qkv[(row_at + h_in) * V8 + LANES + piece];
-                    }
-                    float xa[8], xb[8], wa[8], wb[8];
-                    unpack8(xlo, xa);
-                    unpack8(xhi, xb);
-                    unpack8(w[piece], wa);
-                    unpack8(w[LANES + piece], wb);
-                    float ss = 0.f, dot = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        ss += xa[j] * xa[j] + xb[j] * xb[j];
-                        dot += wa[j] * za[j] * xa[j] + wb[j] * zb[j] * xb[j];
-                    }
-                    const float r = rsqrtf(sum_lanes<LANES>(ss) * (1.f / D) + p.eps);
-                    const float m = sum_lanes<LANES>(dot) * r * (1.f / D);          // mean(w z x r)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float ua = xa[j] * r, ub = xb[j] * r;
-                        const float ta = za[j] * ua, tb = zb[j] * ub;
-                        if (at.kind == 0) { acc[0][j] += ta; acc[0][8 + j] += tb; }
-                        else { acc[1][j] += ta; acc[1][8 + j] += tb; }
-                        za[j] = r * (wa[j] * za[j] - ua * m);
-                        zb[j] = r * (wb[j] * zb[j] - ub * m);
-                    }
+                if (sub == 0) {
+                    float* dst = sums + (warp * 2 + k) * D + (j < 4 ? 0 : D / 2) + piece * 8 + (j & 3) * 2;
+                    dst[0] = x;
+                    dst[1] = y;
                 }
-                lo = pack8(za);
-                hi = pack8(zb);
             }
-            if (!at.live) continue;
-            uint4* dst = p.dx + (row_at + h_in) * V8;
-            dst[piece] = lo;
-            dst[LANES + piece] = hi;
-        }
-    }
-    if (p.wq == nullptr) return;
-    // the CTA's sums, in a fixed order: lanes of the same channels, then warps
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            float x = acc[k][j];
-#pragma unroll
-            for (int off = LANES; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-            if (sub == 0) s_dw[warp][(j < 8 ? 0 : D / 2) + piece * 8 + (j & 7)] = x;
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < D; c += QKN_WARPS * 32) {
+        for (int c = threadIdx.x; c < 2 * D; c += warps * 32) {
             float x = 0.f;
-#pragma unroll
-            for (int w = 0; w < QKN_WARPS; ++w) x += s_dw[w][c];
-            p.part[(static_cast<int64_t>(blockIdx.x) * 2 + k) * D + c] = x;
+            for (int w = 0; w < warps; ++w) x += sums[w * 2 * D + c];
+            p.part[static_cast<int64_t>(blockIdx.x) * 2 * D + c] = x;
         }
-        __syncthreads();
+    }
+    if (!ok) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000LL) {}                                // copies in flight land
+        if (lane == 0) atomicOr(p.dev_status, DEV_WAIT_EXPIRED);
     }
 }
 
@@ -299,17 +422,43 @@ qk_norm_weight_sum_kernel(const float* __restrict__ part, int n, int d, float* _
     }
 }
 
-// Warps per row: one where the rows fill the GPU (32 warps on each SM), else up to one for each group of heads.
-int pick_warps_per_row(int rows, int Hq, int Hkv, int d, int sm_count) {
-    const int per = 32 / (d / 16), groups = (Hq + per - 1) / per + 2 * ((Hkv + per - 1) / per);
-    int w = 1;
-    while (w * 2 <= groups && static_cast<int64_t>(rows) * w < 32LL * sm_count) w *= 2;
-    return w;
+template <int D, int MODE>
+int launch_qk_norm(const QkNormParams& p, int ctas, int warps, cudaStream_t stream) {
+    using S = QkNormShape<MODE>;
+    // (a warp's pass may reach 32 / (D / 16) - 1 heads beyond the last of its stage: read, not used)
+    constexpr int RING = S::STAGES * S::STAGE_BYTES, SMEM = S::WARPS * RING + 1024;
+    static std::atomic<uint64_t> smem_set{0};
+    if (ensure_dynamic_smem(smem_set, qk_norm_kernel<D, MODE>, SMEM) != DARE_OK) return DARE_ERR_CUDA;
+    return launch_kernel(qk_norm_kernel<D, MODE>, dim3(ctas), warps * 32, warps * RING + 1024, stream, 1, p);
+}
+// Items as large as a stage holds, equal shares of a row; smaller ones, down to a warp's pass, where there would be none for some
+// warps.  One CTA per SM, no more than there are items.
+template <int MODE>
+int run_qk_norm(const dare_ctx* ctx, QkNormParams& p, int d, int* ctas, cudaStream_t stream) {
+    using S = QkNormShape<MODE>;
+    const int pass = 32 / (d / 16), most = S::STAGE_BYTES / (d * 2) / (MODE == QKN_BACKWARD ? 2 : 1) / pass * pass, heads = p.Hq + 2 * p.Hkv;
+    int n = (heads + most - 1) / most;
+    const int64_t warps = static_cast<int64_t>(ctx->sm_count) * S::WARPS;
+    while (static_cast<int64_t>(p.rows) * n < warps && n * pass < heads) ++n;
+    p.item_heads = ((heads + n - 1) / n + pass - 1) / pass * pass;
+    p.row_items = (heads + p.item_heads - 1) / p.item_heads;
+    const int64_t items = static_cast<int64_t>(p.rows) * p.row_items;
+    *ctas = static_cast<int>(items < ctx->sm_count ? items : ctx->sm_count);
+    if (MODE == QKN_BACKWARD && p.wq && static_cast<size_t>(*ctas) * 2 * d * sizeof(float) > ctx->workspace_bytes) return DARE_ERR_WORKSPACE;
+    const int64_t share = (items + *ctas - 1) / *ctas;
+    const int warps_cta = static_cast<int>(share < S::WARPS ? share : S::WARPS);
+    return d == 128 ? launch_qk_norm<128, MODE>(p, *ctas, warps_cta, stream) : launch_qk_norm<64, MODE>(p, *ctas, warps_cta, stream);
 }
 
-int backward_ctas(int rows, int warps_per_row, int sm_count) {
-    const int64_t need = (static_cast<int64_t>(rows) * warps_per_row + QKN_WARPS - 1) / QKN_WARPS;
-    return static_cast<int>(need < 2LL * sm_count ? need : 2LL * sm_count);
+QkNormParams make_params(const dare_ctx* ctx, const void* qkv, int rows, int Hq, int Hkv, const void* wq, const void* wk, float eps,
+                         const int32_t* positions, const float* rope, int n_positions) {
+    QkNormParams p = {};
+    p.qkv = static_cast<const __nv_bfloat16*>(qkv);
+    p.rows = rows; p.Hq = Hq; p.Hkv = Hkv; p.eps = eps; p.positions = positions; p.n_positions = n_positions;
+    p.wq = static_cast<const uint4*>(wq); p.wk = static_cast<const uint4*>(wk);
+    p.rope = reinterpret_cast<const float4*>(rope);
+    p.dev_status = ctx->dev_status;
+    return p;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -320,7 +469,7 @@ int check_rows(const dare_ctx* ctx, const void* qkv, int rows, int Hq, int Hkv, 
     if ((wq == nullptr) != (wk == nullptr)) return DARE_ERR_NULL;
     if (int rc = check_current_device(ctx)) return rc;
     if (rows < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (d != 64 && d != 128) || n_positions < 1) return DARE_ERR_SHAPE;
-    if (static_cast<int64_t>(Hq) + 2LL * Hkv > (1 << 20) || rows > (1 << 26)) return DARE_ERR_SHAPE;
+    if (static_cast<int64_t>(Hq) + 2LL * Hkv > (1 << 20) || rows > (1 << 30) / (Hq + 2 * Hkv)) return DARE_ERR_SHAPE;      // (items are 32-bit)
     if (!(eps >= 0.f) || isinf(eps)) return DARE_ERR_RANGE;
     if (!aligned16(qkv) || !aligned16(wq) || !aligned16(wk) || !aligned16(rope)) return DARE_ERR_ALIGN;
     return DARE_OK;
@@ -348,18 +497,10 @@ int dare_qk_norm_rope(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hk
     if (!q_out || !k_out || !v_out) return DARE_ERR_NULL;
     if (int rc = check_rows(ctx, qkv, n_rows, Hq, Hkv, d, q_weight, k_weight, eps, positions, rope_table, n_positions)) return rc;
     if (!aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out)) return DARE_ERR_ALIGN;
-    QkNormParams p = {};
-    p.qkv = static_cast<const uint4*>(qkv);
-    p.rows = n_rows; p.Hq = Hq; p.Hkv = Hkv; p.eps = eps; p.positions = positions; p.n_positions = n_positions;
-    p.wq = static_cast<const uint4*>(q_weight); p.wk = static_cast<const uint4*>(k_weight);
-    p.rope = reinterpret_cast<const float4*>(rope_table);
-    p.q_out = static_cast<uint4*>(q_out); p.k_out = static_cast<uint4*>(k_out); p.v_out = static_cast<uint4*>(v_out);
-    p.dev_status = ctx->dev_status;
-    p.warps_per_row = pick_warps_per_row(n_rows, Hq, Hkv, d, ctx->sm_count);
-    const int64_t items = static_cast<int64_t>(n_rows) * p.warps_per_row;
-    return launch_kernel(d == 128 ? qk_norm_rope_kernel<128, false> : qk_norm_rope_kernel<64, false>,
-                         dim3(static_cast<unsigned>((items + QKN_WARPS - 1) / QKN_WARPS)), QKN_WARPS * 32, 0,
-                         static_cast<cudaStream_t>(stream), 1, p);
+    QkNormParams p = make_params(ctx, qkv, n_rows, Hq, Hkv, q_weight, k_weight, eps, positions, rope_table, n_positions);
+    p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out); p.v_out = static_cast<__nv_bfloat16*>(v_out);
+    int ctas = 0;
+    return run_qk_norm<QKN_DENSE>(ctx, p, d, &ctas, static_cast<cudaStream_t>(stream));
 }
 
 int dare_paged_kv_append(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight,
@@ -371,20 +512,12 @@ int dare_paged_kv_append(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int
     if (int rc = check_rows(ctx, qkv, n_rows, Hq, Hkv, d, q_weight, k_weight, eps, positions, rope_table, n_positions)) return rc;
     if (int rc = check_pages(n_seqs, max_pages, n_pages, page_size, Hkv)) return rc;
     if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(q_out)) return DARE_ERR_ALIGN;
-    QkNormParams p = {};
-    p.qkv = static_cast<const uint4*>(qkv);
-    p.rows = n_rows; p.Hq = Hq; p.Hkv = Hkv; p.eps = eps; p.positions = positions; p.n_positions = n_positions;
-    p.wq = static_cast<const uint4*>(q_weight); p.wk = static_cast<const uint4*>(k_weight);
-    p.rope = reinterpret_cast<const float4*>(rope_table);
-    p.q_out = static_cast<uint4*>(q_out); p.k_out = static_cast<uint4*>(k_pages); p.v_out = static_cast<uint4*>(v_pages);
+    QkNormParams p = make_params(ctx, qkv, n_rows, Hq, Hkv, q_weight, k_weight, eps, positions, rope_table, n_positions);
+    p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_pages); p.v_out = static_cast<__nv_bfloat16*>(v_pages);
     p.seq_ids = seq_ids; p.table = block_table; p.n_seqs = n_seqs; p.max_pages = max_pages; p.n_pages = n_pages;
     p.page_shift = __builtin_ctz(static_cast<unsigned>(page_size));
-    p.dev_status = ctx->dev_status;
-    p.warps_per_row = pick_warps_per_row(n_rows, Hq, Hkv, d, ctx->sm_count);
-    const int64_t items = static_cast<int64_t>(n_rows) * p.warps_per_row;
-    return launch_kernel(d == 128 ? qk_norm_rope_kernel<128, true> : qk_norm_rope_kernel<64, true>,
-                         dim3(static_cast<unsigned>((items + QKN_WARPS - 1) / QKN_WARPS)), QKN_WARPS * 32, 0,
-                         static_cast<cudaStream_t>(stream), 1, p);
+    int ctas = 0;
+    return run_qk_norm<QKN_APPEND>(ctx, p, d, &ctas, static_cast<cudaStream_t>(stream));
 }
 
 int dare_qk_norm_rope_backward(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight,
@@ -396,21 +529,12 @@ int dare_qk_norm_rope_backward(dare_ctx* ctx, const void* qkv, int n_rows, int H
     if (q_weight && (!d_q_weight || !d_k_weight)) return DARE_ERR_NULL;
     if (int rc = check_rows(ctx, qkv, n_rows, Hq, Hkv, d, q_weight, k_weight, eps, positions, rope_table, n_positions)) return rc;
     if (!aligned16(d_q) || !aligned16(d_k) || !aligned16(d_v) || !aligned16(d_qkv)) return DARE_ERR_ALIGN;
-    QkNormGradParams p = {};
-    p.qkv = static_cast<const uint4*>(qkv);
-    p.rows = n_rows; p.Hq = Hq; p.Hkv = Hkv; p.eps = eps; p.positions = positions; p.n_positions = n_positions;
-    p.wq = static_cast<const uint4*>(q_weight); p.wk = static_cast<const uint4*>(k_weight);
-    p.rope = reinterpret_cast<const float4*>(rope_table);
-    p.gq = static_cast<const uint4*>(d_q); p.gk = static_cast<const uint4*>(d_k); p.gv = static_cast<const uint4*>(d_v);
-    p.dx = static_cast<uint4*>(d_qkv);
+    QkNormParams p = make_params(ctx, qkv, n_rows, Hq, Hkv, q_weight, k_weight, eps, positions, rope_table, n_positions);
+    p.gq = static_cast<const __nv_bfloat16*>(d_q); p.gk = static_cast<const __nv_bfloat16*>(d_k); p.gv = static_cast<const __nv_bfloat16*>(d_v);
+    p.dx = static_cast<__nv_bfloat16*>(d_qkv);
     p.part = static_cast<float*>(ctx->workspace);
-    p.dev_status = ctx->dev_status;
-    p.warps_per_row = pick_warps_per_row(n_rows, Hq, Hkv, d, ctx->sm_count);
-    const int ctas = backward_ctas(n_rows, p.warps_per_row, ctx->sm_count);
-    if (q_weight && static_cast<size_t>(ctas) * 2 * d * sizeof(float) > ctx->workspace_bytes) return DARE_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int rc = launch_kernel(d == 128 ? qk_norm_rope_backward_kernel<128> : qk_norm_rope_backward_kernel<64>, dim3(ctas), QKN_WARPS * 32,
-                           0, s, 1, p);
+    int ctas = 0, rc = run_qk_norm<QKN_BACKWARD>(ctx, p, d, &ctas, s);
     if (rc != DARE_OK || !q_weight) return rc;
     return launch_kernel(qk_norm_weight_sum_kernel, dim3(2 * d / DW_COLS), DW_THREADS, 0, s, 1, static_cast<const float*>(p.part), ctas, d,
                          d_q_weight, d_k_weight);
