@@ -15,6 +15,12 @@ int make_tmap_bf16_2d(const dare_ctx* ctx, CUtensorMap* out, const void* base, u
     return make_tmap_bf16_3d(ctx, out, base, rows, 0, cols, box_rows, 0, box_cols);
 }
 
+// (in the cache such a map goes by a middle extent that no other has)
+constexpr uint64_t TMAP_HALVES = ~uint64_t(0);
+int make_tmap_bf16_halves(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+    return make_tmap_bf16_3d(ctx, out, base, rows, TMAP_HALVES, cols, box_rows, static_cast<uint32_t>(cols / 64), 64);
+}
+
 int make_tmap_bf16_3d(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t mid, uint64_t cols,
                       uint32_t box_rows, uint32_t box_mid, uint32_t box_cols) {
     TmapCache::Slot* slot = nullptr;
@@ -47,6 +53,11 @@ int make_tmap_bf16_3d(const dare_ctx* ctx, CUtensorMap* out, const void* base, u
     cuuint64_t dims[3] = {cols, flat ? rows : mid, rows};
     cuuint64_t strides[2] = {cols * 2, cols * mid * 2};   // bytes, dimensions 1 and 2
     cuuint32_t box[3] = {box_cols, flat ? box_rows : box_mid, box_rows};
+    if (mid == TMAP_HALVES) {
+        dims[0] = 64; dims[1] = rows; dims[2] = cols / 64;
+        strides[0] = cols * 2; strides[1] = 128;
+        box[1] = box_rows; box[2] = box_mid;
+    }
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = ctx->encode_tiled(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, flat ? 2 : 3, const_cast<void*>(base), dims, strides,
                                    box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,

@@ -148,6 +148,8 @@ constexpr int PAGED_MAX_CTAS = 1024;
 // bf16 2-D row-major tensor [rows, cols] -> tensor map with a [box_rows, 64] box and 128-byte swizzle.
 int make_tmap_bf16_2d(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols,
                       uint32_t box_rows, uint32_t box_cols);
+// The same with a box of all `cols` (a multiple of 64) columns, which arrive 64 at a time: [cols / 64][box_rows][64].
+int make_tmap_bf16_halves(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 // The same for [rows, mid, cols] with a [box_rows, box_mid, box_cols] box.
 int make_tmap_bf16_3d(const dare_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint64_t mid, uint64_t cols,
                       uint32_t box_rows, uint32_t box_mid, uint32_t box_cols);

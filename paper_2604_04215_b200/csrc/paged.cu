@@ -10,7 +10,7 @@
 //     of its CTAs comes last, in the order of the keys, so that results do not depend on the order of arrival;
 //   * the query rows of all Hq / Hkv heads that share a KV head are one tile of up to 8: a key is read once for them.  (More rows
 //     go to the tcgen05 kernel of attn.cu, see launch_attn_paged_tc);
-//   * a producer warp copies table entries two tiles ahead and streams the tiles through a shared-memory ring with TMA (128-byte
+//   * a producer warp reads table entries 32 at a time, ahead of their turn, and streams the tiles through a shared-memory ring with TMA (128-byte
 //     swizzle; a lane per page piece; pieces that nobody may see are read at a row behind the pool, which TMA fills with zeros);
 //   * four consumer warps own 16 keys of each tile: QK^T and PV on warp-level MMAs (m16n8k16) with the keys and channels as rows and
 //     the query rows as columns, the online softmax in registers.
@@ -30,8 +30,10 @@ constexpr float LN2_F = 0.6931471805599453f;
 constexpr int PG_KT = 64;          // keys per tile
 constexpr int PG_ROWS = 8;         // packed query rows of a unit, at most
 constexpr int PG_WARPS = 4;        // consumers, each with 16 of a tile's keys
-constexpr int PG_LEAST = 3;        // tiles that are a CTA's worth
-constexpr int PG_AHEAD = 2;        // tiles whose pages are looked up before their turn
+// Tiles that the longest unit may have more than a stretch of equal length has, and units still be taken whole: joining costs a CTA
+// 7.4 k cycles at its end, some five tiles' time (32 sequences x 8 heads of 17 or 18 tiles on 296 CTAs: 29.7 us in stretches, 25.4 whole).
+constexpr int PG_LONGER = 5;
+constexpr int PG_UNITS = 8;        // descriptors of units on their way
 
 struct PagedParams {
     int B, L, Hq, Hkv, g, R;              // R = L * g packed query rows per (sequence, KV head)
@@ -50,13 +52,12 @@ struct PagedParams {
 
 enum { TILE_FIRST = 1, TILE_LAST = 2, TILE_END = 4, TILE_MASKED = 8, TILE_NONE = 16 };
 
-// A tile, as the producer hands it to the consumers.
-struct TileDesc {
-    int flags;                // TILE_*: first / last of its unit in this CTA, last of the CTA, some row must not see some key
-    int b, kvh;
-    int key0, n;              // first key, keys of the sequence
-    int first_cta, n_parts;   // the CTAs that share the unit
-    int first_slot;           // the slot of first_cta's part
+// A tile and a unit, as the producer hands them to the consumers.
+struct alignas(16) TileDesc { int flags, key0, unit, unused; };      // TILE_*: first / last of its unit in this CTA, last of the CTA, some
+                                                                     // row must not see some key; first key; place of the unit's descriptor
+struct alignas(16) UnitDesc {
+    int b, kvh, n, parts;      // n: keys of the sequence; parts: CTAs that share the unit
+    int first_cta, slot, first_slot, unused;      // the first of them, where this CTA's part goes, where first_cta's does
 };
 
 template <int STAGES>
@@ -65,10 +66,12 @@ struct PagedBarriers {
     uint64_t empty[STAGES];
     uint64_t merge;
     TileDesc tile[STAGES];
-    TileDesc shared_unit[2];           // units that this CTA shares with others: its first one, its last one
-    int pages[PG_AHEAD + 2][32];       // table entries on their way, per lane of the producer
+    UnitDesc unit[PG_UNITS];
+    UnitDesc shared_unit[2];           // units that this CTA shares with others: its first one, its last one
     uint32_t abort_flag;
     uint32_t arrived[2];
+    // (when a unit's descriptor is written, the tile STAGES + 1 before its first one has been consumed)
+    static_assert(PG_UNITS >= STAGES + 1, "descriptors of units");
 };
 
 template <int D>
@@ -97,15 +100,12 @@ struct SeqTiles {
     __device__ __forceinline__ int key0(int t) const { return (t < n_sink ? t : win_tile + t - n_sink) * PG_KT; }
 };
 
-// The list of all units' tiles cut into stretches of equal length (to one tile), one per CTA: as many as there are CTAs, but of
-// PG_LEAST tiles at least where that does not leave a unit without a CTA of its own.
+// The list of all units' tiles cut into stretches of equal length (to one tile), one per CTA (none where there are fewer tiles).  As
+// many CTAs as that gives even where each then has one tile: a tile after another costs a CTA more than one part more costs those who
+// join them (1 sequence of 777 keys on 52, 26 and 17 CTAs 8.0, 9.7 and 10.8 us).
 struct Stretches {
     int n, each, more;        // CTAs that have one; tiles of each; the first `more` have one tile more
-    __device__ __forceinline__ Stretches(int tiles, int units, int ctas) {
-        n = min(max(units, tiles / PG_LEAST), ctas);
-        each = tiles / n;
-        more = tiles - each * n;
-    }
+    __device__ __forceinline__ Stretches(int tiles, int ctas) : n(min(tiles, ctas)), each(tiles / n), more(tiles - each * n) {}
     __device__ __forceinline__ int begin(int cta) const { return min(cta, n) * each + min(cta, more); }
     __device__ __forceinline__ int cta_of(int tile) const {
         const int longer = more * (each + 1);
@@ -124,21 +124,21 @@ __device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINI
 // two rows at once, and asks for JOIN parts at a time: what this costs is trips to L2, one after the other.
 constexpr int JOIN = 8;
 template <int D>
-__device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc& unit) {
+__device__ __forceinline__ void join_parts(const PagedParams& p, const UnitDesc& unit) {
     constexpr int THREADS = PG_WARPS * 32;
-    const TileDesc u = unit;
+    const UnitDesc u = unit;
     const int items = p.R * (D / 4);
     const float2* part_ml = reinterpret_cast<const float2*>(p.part_ml);
     const float4* part_o = reinterpret_cast<const float4*>(p.part_o);
     for (int item0 = threadIdx.x; item0 < items; item0 += 2 * THREADS) {
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-        for (int k0 = 0; k0 < u.n_parts; k0 += JOIN) {
+        for (int k0 = 0; k0 < u.parts; k0 += JOIN) {
             float2 ml[2][JOIN];
             float4 x[2][JOIN];
 #pragma unroll
             for (int k = 0; k < JOIN; ++k) {
-                const int part = min(k0 + k, u.n_parts - 1);           // (beyond the last: the last one, counted 0 times)
+                const int part = min(k0 + k, u.parts - 1);           // (beyond the last: the last one, counted 0 times)
                 const int slot = (u.first_cta + part) * 2 + (part == 0 ? u.first_slot : 0);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -158,7 +158,7 @@ __device__ __forceinline__ void join_parts(const PagedParams& p, const TileDesc&
                 acc[e].x *= w; acc[e].y *= w; acc[e].z *= w; acc[e].w *= w;
 #pragma unroll
                 for (int k = 0; k < JOIN; ++k) {
-                    if (k0 + k >= u.n_parts) continue;
+                    if (k0 + k >= u.parts) continue;
                     const float wk = fast_exp2(ml[e][k].x - r);
                     l[e] += ml[e][k].y * wk;
                     acc[e].x += x[e][k].x * wk; acc[e].y += x[e][k].y * wk;
@@ -200,24 +200,31 @@ struct PagedSmem {
 template <int D>
 __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorMap* tm_v, const PagedParams& p, const PagedSmem<D>& sm) {
     using S = PagedShape<D>;
-    constexpr int STAGES = S::STAGES, HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2;
+    constexpr int STAGES = S::STAGES, KV_BYTES = PG_KT * D * 2;
     PagedBarriers<STAGES>* bars = sm.bars;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int lane = threadIdx.x & 31;
-    int total = 0, lens = 0;                       // (lens, lane i: keys of sequence (b & ~31) + i)
-    for (int b0 = (p.B - 1) & ~31; b0 >= 0; b0 -= 32) {
-        lens = 0;
-        int nt = 0;
-        if (b0 + lane < p.B) {
-            const int raw = p.kv_lens[b0 + lane];
-            lens = max(0, min(raw, p.max_pages << p.page_shift));
-            if (blockIdx.x == 0 && raw != lens) atomicOr(p.dev_status, DEV_LEN_CLAMPED);
-            nt = SeqTiles(lens, p).n_tiles;
+    int total = 0, longest = 0, lens = 0;          // (lens, lane i: keys of sequence (b & ~31) + i)
+    for (int g0 = 0; g0 < p.B; g0 += 4 * 32) {     // (four loads at a time)
+        int raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = g0 + i * 32 + lane < p.B ? p.kv_lens[g0 + i * 32 + lane] : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (g0 + i * 32 >= p.B) break;
+            const int keys = max(0, min(raw[i], p.max_pages << p.page_shift));
+            if (blockIdx.x == 0 && raw[i] != keys) atomicOr(p.dev_status, DEV_LEN_CLAMPED);
+            const int nt = g0 + i * 32 + lane < p.B ? SeqTiles(keys, p).n_tiles : 0;
+            total += __reduce_add_sync(0xffffffffu, nt);
+            longest = max(longest, __reduce_max_sync(0xffffffffu, nt));
+            if (g0 + i == 0) lens = keys;
         }
-        total += __reduce_add_sync(0xffffffffu, nt);
     }
-    const Stretches st(total * p.Hkv, p.B * p.Hkv, gridDim.x);
-    const int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
+    const Stretches st(total * p.Hkv, gridDim.x);
+    int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
+    // Where there is a CTA for each unit and the longest one is not much longer than a stretch, each takes a unit: nothing to join.
+    const bool unit_each = p.B * p.Hkv <= static_cast<int>(gridDim.x) && longest <= st.each + PG_LONGER;
+    if (unit_each) begin = 0, end = static_cast<int>(blockIdx.x) < p.B * p.Hkv;
     if (begin >= end) {
         if (lane == 0) {
             bars->tile[0].flags = TILE_NONE;
@@ -226,124 +233,140 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         return;
     }
     int b = 0, base = 0;                           // the sequence of tile `begin`; its first tile
-    for (int b0 = 0; b0 < p.B; b0 += 32) {
-        if (b0 > 0) lens = b0 + lane < p.B ? seq_keys(p, b0 + lane) : 0;
-        const int nt = b0 + lane < p.B ? SeqTiles(lens, p).n_tiles : 0;
-        int incl = nt;
+    if (unit_each) {
+        b = static_cast<int>(blockIdx.x) / p.Hkv;
+        if (b >= 32) lens = (b & ~31) + lane < p.B ? seq_keys(p, (b & ~31) + lane) : 0;
+    } else {
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            if (b0 > 0) lens = b0 + lane < p.B ? seq_keys(p, b0 + lane) : 0;
+            const int nt = b0 + lane < p.B ? SeqTiles(lens, p).n_tiles : 0;
+            int incl = nt;
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, incl, off);
-            if (lane >= off) incl += o;
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl += o;
+            }
+            const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * p.Hkv > begin);
+            if (beyond) {
+                const int i = __ffs(beyond) - 1;
+                b = b0 + i;
+                base += __shfl_sync(0xffffffffu, incl - nt, i) * p.Hkv;
+                break;
+            }
+            base += __shfl_sync(0xffffffffu, incl, 31) * p.Hkv;
         }
-        const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * p.Hkv > begin);
-        if (beyond) {
-            const int i = __ffs(beyond) - 1;
-            b = b0 + i;
-            base += __shfl_sync(0xffffffffu, incl - nt, i) * p.Hkv;
-            break;
-        }
-        base += __shfl_sync(0xffffffffu, incl, 31) * p.Hkv;
     }
-    // two cursors over the tiles: `ahead` asks for table entries, `now` follows with the copies
-    struct Cursor {
-        int b, kvh, t, base, lens;
-        SeqTiles sq;
-        __device__ __forceinline__ void next(const PagedParams& p, int lane) {
-            if (++t < sq.n_tiles) return;
-            t = 0;
-            if (++kvh < p.Hkv) return;
+    // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of K or V.  (Both halves of the columns in one copy: a copy takes
+    // its lane some 85 cycles to send, and the 16 of a tile of 16-key pages, 2 KB each, were what its CTA waited for.)
+    const int pp_shift = min(p.page_shift, 6), pieces_shift = 6 - pp_shift, rows_pp = 1 << pp_shift;      // (64 keys a tile)
+    const bool active = lane < 2 << pieces_shift;
+    const int piece = lane & ((1 << pieces_shift) - 1), is_v = lane >> pieces_shift;
+    const int pool_rows = (p.n_pages * p.Hkv) << p.page_shift;
+    const uint32_t dst0 = is_v * KV_BYTES + piece * rows_pp * D * 2;
+    const CUtensorMap* tm = is_v ? tm_v : tm_k;
+    int n = __shfl_sync(0xffffffffu, lens, b & 31), kvh, t;
+    {
+        const int nt = SeqTiles(n, p).n_tiles;
+        kvh = unit_each ? static_cast<int>(blockIdx.x) - b * p.Hkv : (begin - base) / nt;
+        t = unit_each ? 0 : begin - base - kvh * nt;
+        if (unit_each) end = nt;
+    }
+    int stage = 0, unit = 0;
+    uint32_t phase = 0;
+    for (int at = begin; at < end;) {              // unit by unit
+        const SeqTiles sq(n, p);
+        const int count = min(sq.n_tiles - t, end - at);
+        // Table entries 32 pieces at a time, a lane each, the next 32 while these are on their way: the pool row that a piece is read from
+        // (that behind the pool, zeros, for one that nobody may see and for one without a page).
+        const int32_t* table = p.table + static_cast<long long>(b) * p.max_pages;
+        auto key_of = [&](int i) { return sq.key0(t + (i >> pieces_shift)) + ((i & ((1 << pieces_shift) - 1)) << pp_shift); };
+        auto ask = [&](int i, int& page) -> bool {
+            const int key = key_of(i);
+            const bool visible = (i >> pieces_shift) < count && key < n && (key < p.sinks || key + rows_pp > sq.w0);
+            if (visible) page = table[key >> p.page_shift];
+            return visible;
+        };
+        auto row_of = [&](int i, int page, bool visible) -> int {
+            if (!visible) return pool_rows;
+            if (page < 0 || page >= p.n_pages) {
+                atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
+                return pool_rows;
+            }
+            return ((page * p.Hkv + kvh) << p.page_shift) + (key_of(i) & ((1 << p.page_shift) - 1));
+        };
+        int page = 0, page_next = 0;
+        bool seen = ask(lane, page), seen_next = ask(lane + 32, page_next);
+        const bool whole = t == 0 && count == sq.n_tiles;
+        const int unit0 = base + kvh * sq.n_tiles;
+        int rows = row_of(lane, page, seen);
+        bool ok = true;
+        for (int i = 0; i < count; ++i) {
+            const int at_piece = i << pieces_shift;
+            if (i > 0 && (at_piece & 31) == 0) {
+                rows = row_of(at_piece + lane, page_next, seen_next);
+                seen_next = ask(at_piece + 32 + lane, page_next);
+            }
+            const int row = __shfl_sync(0xffffffffu, rows, (at_piece + piece) & 31);
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag));
+            if (!ok) break;
+            uint64_t* full = &bars->full[stage];
+            // (the bytes may arrive before they are expected: the phase ends with the arrival below)
+            if (active) tma_load_3d(sm.tiles + stage * S::STAGE + dst0, tm, full, 0, row, 0);
+            if (i == 0) {
+                if (lane < p.R) {
+                    const int pos = p.L == 1 ? 0 : lane / p.g, h = kvh * p.g + lane - pos * p.g;
+                    bulk_load(sm.q + stage * S::Q_STAGE + lane * S::Q_ROW, p.q + ((static_cast<size_t>(b) * p.L + pos) * p.Hq + h) * D, D * 2, full);
+                }
+                const int c0 = whole ? static_cast<int>(blockIdx.x) : st.cta_of(unit0);
+                const int parts = whole ? 1 : st.cta_of(unit0 + sq.n_tiles - 1) - c0 + 1, first_slot = whole || st.begin(c0) == unit0 ? 0 : 1;
+                if (lane == 0)
+                    bars->unit[unit] = {b, kvh, n, parts, c0, 2 * static_cast<int>(blockIdx.x) + (static_cast<int>(blockIdx.x) == c0 ? first_slot : 0), first_slot, 0};
+            }
+            if (lane == 0) {
+                const int key0 = sq.key0(t + i);
+                int flags = (i == 0 ? TILE_FIRST : 0) | (i == count - 1 ? TILE_LAST : 0) | (at + i == end - 1 ? TILE_END : 0);
+                if (key0 + PG_KT > n || (p.window > 0 && key0 < n - p.window && key0 + PG_KT > p.sinks)) flags |= TILE_MASKED;
+                bars->tile[stage] = {flags, key0, unit, 0};
+                mbar_arrive_expect_tx(full, 2 * KV_BYTES + (i == 0 ? p.R * D * 2 : 0));
+            }
+            __syncwarp();
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        at += count;
+        t = 0;
+        unit = (unit + 1) % PG_UNITS;
+        if (++kvh == p.Hkv) {
             kvh = 0;
             base += sq.n_tiles * p.Hkv;
             ++b;
             if ((b & 31) == 0) lens = b + lane < p.B ? seq_keys(p, b + lane) : 0;
-            if (b < p.B) sq = SeqTiles(__shfl_sync(0xffffffffu, lens, b & 31), p);
+            n = __shfl_sync(0xffffffffu, lens, b & 31);
         }
-    };
-    const SeqTiles sq0(__shfl_sync(0xffffffffu, lens, b & 31), p);
-    const int first_head = (begin - base) / sq0.n_tiles;
-    Cursor now = {b, first_head, begin - base - first_head * sq0.n_tiles, base, lens, sq0};
-    Cursor ahead = now;
-
-    // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of one half of K or V
-    const int pp_shift = min(p.page_shift, 6), pieces_shift = 6 - pp_shift, rows_pp = 1 << pp_shift;      // (64 keys a tile)
-    const bool active = lane < (NHALF * 2) << pieces_shift;
-    const int piece = lane & ((1 << pieces_shift) - 1), half = (lane >> pieces_shift) % NHALF, is_v = (lane >> pieces_shift) / NHALF;
-    const int pool_rows = (p.n_pages * p.Hkv) << p.page_shift;
-    const uint32_t dst0 = is_v * KV_BYTES + half * HALF + piece * rows_pp * 128;
-    const CUtensorMap* tm = is_v ? tm_v : tm_k;
-    // A lane copies its piece's table entry to shared memory PG_AHEAD tiles before it is needed, so that nothing waits for it.
-    auto visible = [&](const Cursor& c, int key) { return key < c.sq.n && (key < p.sinks || key + rows_pp > c.sq.w0); };
-    auto fetch = [&](int at) {
-        if (at < end) {
-            const int key = ahead.sq.key0(ahead.t) + piece * rows_pp;
-            if (active && visible(ahead, key))
-                cp_async_4(&bars->pages[at % (PG_AHEAD + 2)][lane], p.table + static_cast<long long>(ahead.b) * p.max_pages + (key >> p.page_shift));
-            ahead.next(p, lane);
-        }
-        cp_async_commit();
-    };
-#pragma unroll
-    for (int k = 0; k < PG_AHEAD; ++k) fetch(begin + k);
-    int stage = 0, c0 = 0, n_parts = 0, slot0 = 0;
-    uint32_t phase = 0;
-    for (int at = begin; at < end; ++at) {
-        fetch(at + PG_AHEAD);
-        const bool first = now.t == 0 || at == begin;
-        if (!__all_sync(0xffffffffu, mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag))) break;
-        uint64_t* full = &bars->full[stage];
-        const int key0 = now.sq.key0(now.t), key = key0 + piece * rows_pp;
-        cp_async_wait<PG_AHEAD>();
-        if (active) {
-            int row = pool_rows;                   // behind the pool: zeros
-            if (visible(now, key)) {
-                const int page = bars->pages[at % (PG_AHEAD + 2)][lane];
-                if (page >= 0 && page < p.n_pages) row = ((page * p.Hkv + now.kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
-                else atomicOr(p.dev_status, DEV_INDEX_OUTSIDE);
-            }
-            // (the bytes may arrive before they are expected: the phase ends with the arrival below)
-            tma_load_2d(sm.tiles + stage * S::STAGE + dst0, tm, full, half * 64, row);
-        }
-        uint32_t bytes = 2 * KV_BYTES;
-        if (first) {
-            if (lane < p.R) {
-                const int i = lane / p.g, h = now.kvh * p.g + lane - i * p.g;
-                bulk_load(sm.q + stage * S::Q_STAGE + lane * S::Q_ROW, p.q + ((static_cast<size_t>(now.b) * p.L + i) * p.Hq + h) * D, D * 2, full);
-            }
-            bytes += p.R * D * 2;
-            const int u0 = now.base + now.kvh * now.sq.n_tiles;
-            c0 = st.cta_of(u0);
-            n_parts = st.cta_of(u0 + now.sq.n_tiles - 1) - c0 + 1;
-            slot0 = st.begin(c0) == u0 ? 0 : 1;
-        }
-        if (lane == 0) {
-            const int n = now.sq.n;
-            TileDesc d;
-            d.flags = (first ? TILE_FIRST : 0) | (now.t == now.sq.n_tiles - 1 || at == end - 1 ? TILE_LAST : 0) | (at == end - 1 ? TILE_END : 0);
-            if (key0 + PG_KT > n || (p.window > 0 && key0 < n - p.window && key0 + PG_KT > p.sinks)) d.flags |= TILE_MASKED;
-            d.b = now.b; d.kvh = now.kvh; d.key0 = key0; d.n = n;
-            d.first_cta = c0; d.n_parts = n_parts; d.first_slot = slot0;
-            bars->tile[stage] = d;
-            mbar_arrive_expect_tx(full, bytes);
-        }
-        __syncwarp();
-        now.next(p, lane);
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
     }
 }
 
 // What a window hides: key j is hidden from query i (at position n - L + i) if sinks <= j < start + i.
 __device__ __forceinline__ int window_start(const PagedParams& p, int n) { return p.window > 0 ? n - p.L - p.window + 1 : -p.L; }
 
-// V rows that no query may see hold whatever lies there: zeroes those of this warp's keys [koff, koff + KPW) of a tile, so that
+// A tile's pieces of pages lie one after the other, in each the halves of its columns.  Where the 16 keys from koff on begin in the first
+// half (they are in one piece); the second half is a piece's rows further.
+__device__ __forceinline__ int slice_at(const PagedParams& p, int koff, int row_bytes) {
+    const int pp = min(p.page_shift, 6);
+    return (koff >> pp << pp) * row_bytes + (koff & ((1 << pp) - 1)) * 128;
+}
+__device__ __forceinline__ int half_stride(const PagedParams& p) { return 128 << min(p.page_shift, 6); }
+
+// V rows that no query may see hold whatever lies there: zeroes those among the 16 keys from key0 on, which `at` holds, so that
 // probability 0 times garbage cannot make a NaN.
-template <int KPW, int NHALF>
-__device__ __forceinline__ void clear_unseen(const PagedParams& p, const TileDesc& ti, uint8_t* vt, int koff) {
-    const int lane = threadIdx.x & 31, start = window_start(p, ti.n);
+template <int NHALF>
+__device__ __forceinline__ void clear_unseen(const PagedParams& p, int key0, int n, uint8_t* at) {
+    const int lane = threadIdx.x & 31, start = window_start(p, n);
     bool wrote = false;
-    for (int o = lane; o < KPW * 8 * NHALF; o += 32) {
-        const int row = koff + (o >> 3) % KPW, half = (o >> 3) / KPW, key = ti.key0 + row;
-        if (key >= ti.n || (key >= p.sinks && key < start)) {
-            *reinterpret_cast<uint4*>(vt + half * PG_KT * 128 + row * 128 + (o & 7) * 16) = make_uint4(0, 0, 0, 0);
+    for (int o = lane; o < 16 * 8 * NHALF; o += 32) {
+        const int row = (o >> 3) % 16, half = (o >> 3) / 16, key = key0 + row;
+        if (key >= n || (key >= p.sinks && key < start)) {
+            *reinterpret_cast<uint4*>(at + half * half_stride(p) + row * 128 + (o & 7) * 16) = make_uint4(0, 0, 0, 0);
             wrote = true;
         }
     }
@@ -356,17 +379,19 @@ __device__ __forceinline__ void clear_unseen(const PagedParams& p, const TileDes
 // channels) quad and quad + 8 of each 16, query rows 2 tq and 2 tq + 1.  A warp owns 16 keys of each tile.
 template <int D>
 struct FewRows {
-    static constexpr int HALF = PG_KT * 128, NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KS = PG_WARPS, KPW = PG_KT / KS;
+    static constexpr int NHALF = D / 64, KV_BYTES = PG_KT * D * 2, KS = PG_WARPS, KPW = PG_KT / KS;
     static_assert(KPW == 16 && PG_ROWS == 8, "a slice is one MMA's keys, the rows are its columns");
     uint32_t qb[D / 16][2];
     float o[D / 16][4];
     float m[2], l[2];
     int row_i[2];              // block positions of this lane's two rows
+    int half;                  // bytes from one half of the columns to the other
 
     __device__ __forceinline__ explicit FewRows(const PagedParams& p) {
         const int tq = threadIdx.x & 3;
         row_i[0] = p.L == 1 ? 0 : 2 * tq / p.g;
         row_i[1] = p.L == 1 ? 0 : (2 * tq + 1) / p.g;
+        half = half_stride(p);
     }
     __device__ __forceinline__ void first(const uint8_t* q_rows) {
         const int lane = threadIdx.x & 31;
@@ -378,20 +403,19 @@ struct FewRows {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
     }
-    __device__ __forceinline__ void tile(const PagedParams& p, const TileDesc& ti, uint8_t* kt, int ks) {
+    __device__ __forceinline__ void tile(const PagedParams& p, bool masked, int key0, int n, uint8_t* kt, int ks) {
         const int lane = threadIdx.x & 31, quad = lane >> 2, koff = ks * KPW;
-        uint8_t* vt = kt + KV_BYTES;
-        const uint32_t kbase = smem_u32(kt), vbase = smem_u32(vt);
-        const bool masked = ti.flags & TILE_MASKED;
-        if (masked) clear_unseen<KPW, NHALF>(p, ti, vt, koff);
+        uint8_t* slice = kt + slice_at(p, koff, D * 2);
+        const uint32_t kbase = smem_u32(slice), vbase = kbase + KV_BYTES;
+        if (masked) clear_unseen<NHALF>(p, key0 + koff, n, slice + KV_BYTES);
         float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};          // (two chains of products)
         {
-            const int key = koff + (lane & 15);
+            const int key = lane & 15;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const int ch = 2 * kk + (lane >> 4);
+                const int ch = 2 * (kk & 3) + (lane >> 4);
                 uint32_t a[4];
-                ldmatrix_x4(kbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
+                ldmatrix_x4(kbase + (kk >> 2) * half + key * 128 + ((ch ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
                 if (kk & 1) mma_bf16_16816(s2, a, qb[kk][0], qb[kk][1]);
                 else mma_bf16_16816(s, a, qb[kk][0], qb[kk][1]);
             }
@@ -399,11 +423,11 @@ struct FewRows {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += s2[e];
         if (masked) {
-            const int start = window_start(p, ti.n);
+            const int start = window_start(p, n);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int key = ti.key0 + koff + quad + (e >> 1) * 8;
-                if (key >= ti.n || (key >= p.sinks && key < start + row_i[e & 1])) s[e] = -INFINITY;
+                const int key = key0 + koff + quad + (e >> 1) * 8;
+                if (key >= n || (key >= p.sinks && key < start + row_i[e & 1])) s[e] = -INFINITY;
             }
         }
         const float c = p.scale_log2;
@@ -437,23 +461,25 @@ struct FewRows {
         l[0] += w[0] + w[2];
         l[1] += w[1] + w[3];
         const uint32_t p0 = movmatrix_trans(pack_bf16(w[0], w[1])), p1 = movmatrix_trans(pack_bf16(w[2], w[3]));
-        const int key = koff + (lane & 7) + (lane >> 4) * 8;
+        const int key = (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            const int ch = 2 * i + ((lane >> 3) & 1);
+            const int ch = 2 * (i & 3) + ((lane >> 3) & 1);
             uint32_t a[4];
-            ldmatrix_x4_trans(vbase + (ch >> 3) * HALF + key * 128 + (((ch & 7) ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
+            ldmatrix_x4_trans(vbase + (i >> 2) * half + key * 128 + ((ch ^ (key & 7)) << 4), a[0], a[1], a[2], a[3]);
             mma_bf16_16816(o[i], a, p0, p1);
         }
     }
     // The unit's end in this CTA: every warp lays its part down over its own keys of the tile that it has just read, then the rows are
     // added up four channels at a time.  `kt` is the tile's place, ml [KS][8].
     template <typename Sync>
-    __device__ __forceinline__ bool finish(const PagedParams& p, const TileDesc& ti, uint8_t* kt, float2* ml, int ks, int slot, Sync&& sync) {
+    __device__ __forceinline__ bool finish(const PagedParams& p, const UnitDesc& u, uint8_t* kt, float2* ml, int ks, Sync&& sync) {
         // place of row q of slice s: pieces of 16 keys of one half of K or V are 2 KB; 8 / (2 NHALF) rows in each
         constexpr int PER = 8 / (2 * NHALF);
         auto at = [&](int s, int q) {
-            return reinterpret_cast<float*>(kt + (q / PER) * HALF + s * KPW * 128 + (q % PER) * (D * 4 + 16) + (q / PER) * (PER * 16));
+            const int k = q / PER;
+            return reinterpret_cast<float*>(kt + slice_at(p, s * KPW, D * 2) + (k / NHALF) * KV_BYTES + (k % NHALF) * half + (q % PER) * (D * 4 + 16) +
+                                            k * (PER * 16));
         };
         const int lane = threadIdx.x & 31, quad = lane >> 2, tq = lane & 3;
 #pragma unroll
@@ -470,7 +496,7 @@ struct FewRows {
             }
         }
         if (!sync()) return false;
-        const bool whole = ti.n_parts == 1;
+        const bool whole = u.parts == 1;
         for (int item = threadIdx.x; item < p.R * (D / 4); item += KS * 32) {
             const int q = item / (D / 4), c4 = item % (D / 4);
             float2 part[KS];
@@ -491,13 +517,13 @@ struct FewRows {
             }
             if (whole) {
                 const float inv = inverse_sum(sum);
-                const int i = p.L == 1 ? 0 : q / p.g, h = ti.kvh * p.g + q - i * p.g;
-                *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(ti.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
+                const int i = p.L == 1 ? 0 : q / p.g, h = u.kvh * p.g + q - i * p.g;
+                *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(u.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
                     make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (p.lse != nullptr && c4 == 0) p.lse[(static_cast<size_t>(ti.b) * p.Hq + h) * p.L + i] = log_sum(top, sum);
+                if (p.lse != nullptr && c4 == 0) p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(top, sum);
             } else {
-                *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * 8 + q) * D + c4 * 4) = acc;
-                if (c4 == 0) reinterpret_cast<float2*>(p.part_ml)[slot * 8 + q] = make_float2(top, sum);
+                *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(u.slot) * PG_ROWS + q) * D + c4 * 4) = acc;
+                if (c4 == 0) reinterpret_cast<float2*>(p.part_ml)[u.slot * PG_ROWS + q] = make_float2(top, sum);
             }
         }
         return true;
@@ -536,6 +562,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         produce<D>(&tm_k, &tm_v, p, sm);
     } else {
         FewRows<D> c(p);
+        UnitDesc u = {};
         int stage = 0, n_shared = 0;
         uint32_t phase = 0, merge_phase = 0, parity = 0;
         // a barrier among the consumer warps, bounded as all waits are
@@ -551,8 +578,11 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             const TileDesc ti = bars->tile[stage];
             if (ti.flags & TILE_NONE) break;
             uint8_t* kt = sm.tiles + stage * S::STAGE;
-            if (ti.flags & TILE_FIRST) c.first(sm.q + stage * S::Q_STAGE);
-            c.tile(p, ti, kt, warp);
+            if (ti.flags & TILE_FIRST) {
+                u = bars->unit[ti.unit];
+                c.first(sm.q + stage * S::Q_STAGE);
+            }
+            c.tile(p, ti.flags & TILE_MASKED, ti.key0, u.n, kt, warp);
             const int this_stage = stage;
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
             if (!(ti.flags & TILE_LAST)) {
@@ -560,26 +590,25 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 if (lane == 0) mbar_arrive(&bars->empty[this_stage]);
                 continue;
             }
-            const int slot = blockIdx.x * 2 + (static_cast<int>(blockIdx.x) == ti.first_cta ? ti.first_slot : 0);
-            if (!c.finish(p, ti, kt, sm.ml + parity * NCW * PG_ROWS, warp, slot, merge_sync)) break;
+            if (!c.finish(p, u, kt, sm.ml + parity * NCW * PG_ROWS, warp, merge_sync)) break;
             parity ^= 1;                                       // (a warp may be a unit ahead of one that still reads its sums)
             fence_proxy_async_smem();                          // (the next copy into this place is the producer's)
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->empty[this_stage]);
             // a shared unit's part has been written; who comes last is found out once, when this CTA has read all its tiles
-            if (ti.n_parts > 1) {
+            if (u.parts > 1) {
                 const int k = (ti.flags & TILE_END) ? 1 : 0;   // (in between units are whole)
-                if (threadIdx.x == 0) bars->shared_unit[k] = ti;
+                if (threadIdx.x == 0) bars->shared_unit[k] = u;
                 n_shared |= 1 << k;
             }
             if (!(ti.flags & TILE_END)) continue;
             if (n_shared) {
                 if (!merge_sync()) break;
                 if (threadIdx.x < 2 && (n_shared >> threadIdx.x & 1)) {
-                    const TileDesc& u = bars->shared_unit[threadIdx.x];
-                    const bool last = atomic_inc_acq_rel(&p.counters[u.first_cta]) == static_cast<uint32_t>(u.n_parts) - 1;
+                    const UnitDesc& s = bars->shared_unit[threadIdx.x];
+                    const bool last = atomic_inc_acq_rel(&p.counters[s.first_cta]) == static_cast<uint32_t>(s.parts) - 1;
                     bars->arrived[threadIdx.x] = last;
-                    if (last) p.counters[u.first_cta] = 0;         // for the next launch
+                    if (last) p.counters[s.first_cta] = 0;         // for the next launch
                 }
                 if (!merge_sync()) break;
                 for (int k = 0; k < 2; ++k)
@@ -659,8 +688,8 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     CUtensorMap tm_k, tm_v;
     const uint64_t pool_rows = static_cast<uint64_t>(n_pages) * Hkv * page_size;
     const uint32_t box_rows = static_cast<uint32_t>(page_size < PG_KT ? page_size : PG_KT);
-    int rc = make_tmap_bf16_2d(ctx, &tm_k, k_pages, pool_rows, d, box_rows, 64);
-    if (rc == DARE_OK) rc = make_tmap_bf16_2d(ctx, &tm_v, v_pages, pool_rows, d, box_rows, 64);
+    int rc = make_tmap_bf16_halves(ctx, &tm_k, k_pages, pool_rows, d, box_rows);
+    if (rc == DARE_OK) rc = make_tmap_bf16_halves(ctx, &tm_v, v_pages, pool_rows, d, box_rows);
     if (rc != DARE_OK) return rc;
     const int n = static_cast<int>(ctas);
     return d == 128 ? launch_paged<128>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64>(ctx, tm_k, tm_v, p, n, s);

@@ -348,6 +348,17 @@ def test_attend_many_sequences(ctx, L):
     _check_attend(out, lse, q, kp, vp, table, lens, 0, 0)
 
 
+@pytest.mark.parametrize("B,hkv,lo,hi,window,sinks", [(70, 4, 600, 700, 0, 0), (35, 8, 100, 5000, 200, 4), (140, 2, 64, 300, 0, 0), (9, 1, 1, 20, 0, 0)])
+def test_attend_units_of_like_length(ctx, B, hkv, lo, hi, window, sinks):
+    """Units that each get a CTA of their own, in the first 32 sequences and behind them, empty places among them."""
+    rng = np.random.default_rng(B)
+    lens = [0 if i % 13 == 6 else int(n) for i, n in enumerate(rng.integers(lo, hi, B))]
+    q, kp, vp, table = _attend_case(B, B, 1, 2 * hkv, hkv, 64, 16, lens, window, sinks)
+    out, lse = _attend(ctx, q, kp, vp, table, lens, window, sinks)
+    assert ctx.device_status() == 0
+    _check_attend(out, lse, q, kp, vp, table, lens, window, sinks)
+
+
 def test_attend_scale_shared_pages_and_no_lse(ctx):
     lens = [200, 150, 200]
     q, kp, vp, table = _attend_case(1, 3, 1, 8, 2, 128, 16, lens, 0, 0, plant=False)
