@@ -755,15 +755,18 @@ def dare_rope_table(ctx: Context, n_positions: int, head_dim: int, base: float =
 def dare_qk_norm_rope(ctx: Context, qkv, positions, rope_table, n_kv_heads: int, q_weight=None, k_weight=None, eps: float = 1e-6,
                       q_out=None, k_out=None, v_out=None, stream=None, check: bool = True):
     """Norms of q and k per head, rotation: (q [rows, Hq, d], k [rows, Hkv, d], v [rows, Hkv, d])."""
-    rows, d, hkv = qkv.shape[0], 2 * rope_table.shape[1], int(n_kv_heads)
-    hq = _fused_heads(qkv.shape[1], hkv, d)
     bf, dev = torch.bfloat16, torch.cuda.current_device()
-    q_out = torch.empty(rows, hq, d, dtype=bf, device=qkv.device) if q_out is None else q_out
-    k_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if k_out is None else k_out
-    v_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if v_out is None else v_out
+    if q_out is None or k_out is None or v_out is None:
+        rows, d, hkv = qkv.shape[0], 2 * rope_table.shape[1], int(n_kv_heads)
+        hq = _fused_heads(qkv.shape[1], hkv, d)
+        q_out = torch.empty(rows, hq, d, dtype=bf, device=qkv.device) if q_out is None else q_out
+        k_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if k_out is None else k_out
+        v_out = torch.empty(rows, hkv, d, dtype=bf, device=qkv.device) if v_out is None else v_out
     rc = _native().qk_norm_rope(ctx.handle.value, dev, _raw(stream, dev), qkv, positions, rope_table, q_weight, k_weight, eps, q_out,
-                                k_out, v_out)
+                                k_out, v_out) if n_kv_heads == k_out.shape[1] else None
     if rc is None:
+        rows, d, hkv = qkv.shape[0], 2 * rope_table.shape[1], int(n_kv_heads)
+        hq = _fused_heads(qkv.shape[1], hkv, d)
         _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
         _same("positions", positions, rows)
         _same("rope_table", rope_table, rope_table.shape[0], d // 2, 2)
@@ -784,18 +787,18 @@ def dare_qk_norm_rope(ctx: Context, qkv, positions, rope_table, n_kv_heads: int,
 def dare_qk_norm_rope_backward(ctx: Context, qkv, positions, rope_table, d_q, d_k, d_v, q_weight=None, k_weight=None, eps: float = 1e-6,
                                d_qkv=None, d_q_weight=None, d_k_weight=None, stream=None, check: bool = True):
     """Gradient of dare_qk_norm_rope: (d_qkv, d_q_weight, d_k_weight); the last two None without weights."""
-    rows, hq, d = d_q.shape
-    hkv = d_k.shape[1]
     bf, f32, dev = torch.bfloat16, torch.float32, torch.cuda.current_device()
     d_qkv = torch.empty_like(qkv) if d_qkv is None else d_qkv
     if q_weight is None:
         d_q_weight = d_k_weight = None
     else:
-        d_q_weight = torch.empty(d, dtype=f32, device=qkv.device) if d_q_weight is None else d_q_weight
-        d_k_weight = torch.empty(d, dtype=f32, device=qkv.device) if d_k_weight is None else d_k_weight
+        d_q_weight = torch.empty(d_q.shape[2], dtype=f32, device=qkv.device) if d_q_weight is None else d_q_weight
+        d_k_weight = torch.empty(d_q.shape[2], dtype=f32, device=qkv.device) if d_k_weight is None else d_k_weight
     rc = _native().qk_norm_rope_backward(ctx.handle.value, dev, _raw(stream, dev), qkv, positions, rope_table, d_q, d_k, d_v, q_weight,
                                          k_weight, eps, d_qkv, d_q_weight, d_k_weight)
     if rc is None:
+        rows, hq, d = d_q.shape
+        hkv = d_k.shape[1]
         _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
         _same("positions", positions, rows)
         _same("rope_table", rope_table, rope_table.shape[0], d // 2, 2)
@@ -816,15 +819,16 @@ def dare_qk_norm_rope_backward(ctx: Context, qkv, positions, rope_table, d_q, d_
 def dare_paged_kv_append(ctx: Context, qkv, seq_ids, positions, block_table, k_pages, v_pages, rope_table, q_weight=None, k_weight=None,
                          eps: float = 1e-6, q_out=None, stream=None, check: bool = True):
     """Norms of q and k per head, rotation, k and v into their pages; returns q [rows, Hq, d].  Rows with seq_ids < 0 are left out."""
-    n_pages, hkv, page, d = k_pages.shape
-    rows = qkv.shape[0]
-    hq = _fused_heads(qkv.shape[1], hkv, d)
     bf, i32, dev = torch.bfloat16, torch.int32, torch.cuda.current_device()
     if q_out is None:
-        q_out = torch.empty(rows, hq, d, dtype=bf, device=qkv.device)
+        _, hkv, _, d = k_pages.shape
+        q_out = torch.empty(qkv.shape[0], _fused_heads(qkv.shape[1], hkv, d), d, dtype=bf, device=qkv.device)
     rc = _native().paged_kv_append(ctx.handle.value, dev, _raw(stream, dev), qkv, seq_ids, positions, block_table, k_pages, v_pages,
                                    rope_table, q_weight, k_weight, eps, q_out)
     if rc is None:
+        n_pages, hkv, page, d = k_pages.shape
+        rows = qkv.shape[0]
+        hq = _fused_heads(qkv.shape[1], hkv, d)
         _same("qkv", qkv, rows, (hq + 2 * hkv) * d)
         _same("seq_ids", seq_ids, rows)
         _same("positions", positions, rows)

@@ -3,7 +3,8 @@
 Bars, from the arithmetic (bf16 inputs taken as they are; half a bf16 step is 2^-8 relative):
   * norms and rotation: one rounding at the end, 2^-8 |ref|.  In front of it: the sum of d <= 128 squares, its root, the products and the
     angles' rounding cost less than 2^-20 relative of each of the two terms of a rotation.
-  * attention: the weights are rounded to bf16 in front of the second product, 2^-8 sum_j p_j |v_j|; the output, 2^-8 |o|; scores
+  * attention: the weights are rounded to bf16 in front of the second product, 2^-8 sum_j p_j |v_j| (up to 8 query rows per KV head: as two
+    bf16 values, 2^-16); the output, 2^-8 |o|; scores
     are fp32 sums of d products, off by at most d 2^-24 max_j scale sum_c |q_c k_jc| (= s), and so are logarithms of weights and
     lse; e^(2s) - 1 <= 3 s of sum_j p_j |v_j|.  The exponential (2^-22), sums over keys and joins: 2^-16 (they are fp32 sums of at most 2^7 parts
     of a tile's 64 keys in turn).
@@ -229,7 +230,8 @@ def _check_attend(out, lse, q, kp, vp, table, lens, window, sinks, scale=0.0):
     ro, rl, pv, sabs = P.attn_paged(f64(q), f64(kp), f64(vp), table, lens, window, sinks, scale)
     d = q.shape[-1]
     s = d * 2.0 ** -24 * sabs                                            # [B, Hq, L]
-    cost = np.swapaxes(3 * s, 1, 2)[..., None] + HALF + 2.0 ** -16
+    few = q.shape[1] * q.shape[2] // kp.shape[1] <= 8
+    cost = np.swapaxes(3 * s, 1, 2)[..., None] + (2.0 ** -16 if few else HALF) + 2.0 ** -16
     bound = HALF * np.abs(ro) * (1 + HALF) + cost * pv + 1e-30
     got = _np(out)
     assert np.isfinite(got).all()
