@@ -482,7 +482,9 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  *   behind n, are not read and their table entries may be anything; a page outside [0, n_pages) that one can see reads as zeros and
  *   sets DARE_DEV_INDEX_OUTSIDE.  Cached values that some query of a block sees must be finite for all of its queries.
  *   Results do not depend on the order in which the GPU runs the parts.  Supported: Hq % Hkv == 0, Hq / Hkv <= 128, d in {64, 128},
- *   L >= 1, L * Hq / Hkv <= 2^20; ctx workspace of 128 * (d + 2) bytes for each SM.
+ *   L >= 1, L * Hq / Hkv <= 2^20, B * Hkv <= 65535 where that is more than 8; ctx workspace of 128 * (d + 2) bytes for each SM.
+ *   n may be smaller than L (the positions of the first queries are then negative, the rule of what is visible stays).
+ * Outputs of these calls do not overlap their inputs.
  */
 int dare_rope_table(dare_ctx* ctx, int n_positions, int d, double base, float* table, void* stream);
 int dare_qk_norm_rope(dare_ctx* ctx, const void* qkv, int n_rows, int Hq, int Hkv, int d, const void* q_weight, const void* k_weight,

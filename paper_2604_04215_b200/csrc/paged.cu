@@ -671,7 +671,10 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     // Up to PG_ROWS packed query rows take the kernel of this file, more the tcgen05 kernel.  us here / there: 7 rows, 1 sequence of 8000
     // keys 16.4 / 16.9, 18 of 2000 19.5 / 21.3, 74 of 1000 29.1 / 32.5.  With the rows as the MMA's 16 rows instead of its 8 columns, 9
     // to 16 rows took 25.6 / 17.3, 22.4 / 21.3 and 31.4 / 32.7, and 32 rows 46 / 17.5, 38 / 21.6 and 39.5 / 33.4.
-    if (L * (Hq / Hkv) > PG_ROWS) return launch_attn_paged_tc(ctx, a, s);
+    if (L * (Hq / Hkv) > PG_ROWS) {
+        if (static_cast<long long>(B) * Hkv > 65535) return DARE_ERR_SHAPE;      // (a grid's second dimension)
+        return launch_attn_paged_tc(ctx, a, s);
+    }
 
     PagedParams p = {};
     p.B = B; p.L = L; p.Hq = Hq; p.Hkv = Hkv; p.g = Hq / Hkv; p.R = L * p.g;

@@ -277,6 +277,11 @@ def _attend(ctx, q, kp, vp, table, lens, window, sinks, lse=True, **kw):
     (4, 8, 8, 64, 16, [400, 65], 1, 1),
     (32, 28, 4, 128, 16, [512, 40], 48, 4),
     (40, 4, 2, 64, 64, [512, 40], 7, 130),
+    (1, 128, 1, 64, 16, [100, 3], 0, 0),                     # as many heads on one as a tile has rows, and a few less
+    (3, 100, 1, 128, 32, [77, 3], 20, 2),
+    (4, 4, 2, 64, 16, [2, 1, 3, 4], 0, 0),                   # fewer keys than queries
+    (4, 4, 2, 64, 16, [2, 1, 3, 70], 2, 1),
+    (40, 4, 2, 64, 16, [39, 1, 90], 3, 1),
     (2, 4, 4, 64, 16, [90], 90, 3),
     (2, 4, 4, 64, 16, [90], 2 ** 31 - 1, 2 ** 31 - 1),
 ])
@@ -561,6 +566,7 @@ def test_refusals(ctx):
     for empty in (dict(q=(0, 1, 4, 64), table=(0, 3)), dict(q=(2, 0, 4, 64)), dict(table=(2, 0)), dict(pool=(0, 2, 16, 64))):
         assert attend(**empty) == -1                         # (an empty tensor has no address)
     assert attend(q=(2, 1, 258, 64)) == -2                   # 129 query heads per KV head
+    assert attend(q=(40000, 9, 2, 64), table=(40000, 1)) == -2      # more (sequence, KV head) pairs of more than 8 rows than a grid has
     assert attend(window=-1) == -4 and attend(sinks=-1) == -4 and attend(scale=-1.0) == -4 and attend(scale=float("nan")) == -4
     assert attend(scale=float("inf")) == -4
     rope = torch.zeros(10, 32, 2, device="cuda")
