@@ -190,8 +190,9 @@ __device__ __forceinline__ void bulk_store(void* dst, const void* smem_src, uint
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(smem_src)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// Until this thread's groups have been read from shared memory / are complete.
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// Until all but N of this thread's groups have been read from shared memory / all are complete.
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // Asks for a tile to be brought into L2 (no shared-memory destination, nothing to wait for): issued a few
 // pipeline steps ahead of the load, it takes the HBM latency off the shared-memory ring.

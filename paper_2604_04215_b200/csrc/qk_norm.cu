@@ -22,14 +22,15 @@ namespace {
 
 enum { QKN_DENSE = 0, QKN_APPEND = 1, QKN_BACKWARD = 2 };
 
-// One CTA per SM.  Stage: of an item's run of heads, in the backward pass of values and of gradients.  us at 19201 rows of 28 + 4 + 4
-// heads of 128, forward / backward, for 12 warps x 2 stages of 9216 bytes 67.9 / 89.5, 16 x 3 of 4608 57.6 / 151.5 (128 registers: spills), 12 x 3
-// of 6144 67.4 / 90.8, 16 x 2 of 6144 68.9 / 112.9, 8 x 3 of 9216 64.9 / 96.1, 24 x 2 of 4608 116 / 211.
+// One CTA per SM.  Stages of an item's run of heads, in the backward pass of values and of gradients: one that is worked on, the next one,
+// one on its way out.  As fast as a plain copy of the same bytes is here (4310 rows of 32 + 32 + 32 heads of 128 36.6 us, copied 36.7;
+// 19201 of 28 + 4 + 4 57 to 61, copied 61.4); 12 and 14 warps with larger stages 60 to 66 there.  The backward pass spills with 16 warps'
+// 128 registers: 151 us instead of 88.
 template <int MODE>
 struct QkNormShape {
     static constexpr int WARPS = MODE == QKN_BACKWARD ? 12 : 16;             // at most
-    static constexpr int STAGES = MODE == QKN_BACKWARD ? 2 : 3;
-    static constexpr int STAGE_BYTES = MODE == QKN_BACKWARD ? 9216 : 4608;
+    static constexpr int STAGES = 3;
+    static constexpr int STAGE_BYTES = MODE == QKN_BACKWARD ? 6144 : 4608;
 };
 
 struct QkNormParams {
@@ -265,13 +266,10 @@ qk_norm_kernel(const QkNormParams p) {
     uint64_t acc[2][8];                                                      // the weights' gradients, pairs of channels
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = 0;
-    for (int s = 0; s < QKN_STAGES - 1; ++s) {
-        if (lane == 0 && ahead.row < p.rows) send_for(ahead, s);
-        ahead.next();
-    }
+    if (lane == 0 && ahead.row < p.rows) send_for(ahead, 0);
+    ahead.next();
     // What an item needs besides its heads is asked for ahead of it, so that nothing waits for it: its position (and sequence) two
-    // items before, its angles (and page) one item before.  (In the backward pass the angles that wait would spill: 106 us instead of 95 at
-    // 19201 rows of 28 + 4 + 4 heads of 128.)
+    // items before, its angles (and page) one item before.  (In the backward pass the angles that wait would spill: 106 us instead of 95.)
     struct Place { int pos, seq; };
     auto place_of = [&](const ItemWalk& w) -> Place {
         return w.row < p.rows ? Place{p.positions[w.row], APPEND ? p.seq_ids[w.row] : 0} : Place{-1, -1};
@@ -309,10 +307,10 @@ qk_norm_kernel(const QkNormParams p) {
         Angles angles1 = {};
         if (BACK) angles = angles_of(place);
         else angles1 = angles_of(place1);
-        // the next item takes the last one's place, once its copies out have read it
-        bulk_wait_read();
+        // the next item takes the place of the last but one, once the copies out of that have read it
+        bulk_wait_read<1>();
         __syncwarp();
-        if (lane == 0 && ahead.row < p.rows) send_for(ahead, stage == 0 ? QKN_STAGES - 1 : stage - 1);
+        if (lane == 0 && ahead.row < p.rows) send_for(ahead, stage == QKN_STAGES - 1 ? 0 : stage + 1);
         ahead.next();
         uint64_t cs[4], sn[4];
 #pragma unroll
