@@ -237,7 +237,7 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
     if (unit_each) {
         b = static_cast<int>(blockIdx.x) / p.Hkv;
         if (b >= 32) lens = (b & ~31) + lane < p.B ? seq_keys(p, (b & ~31) + lane) : 0;
-    } else {
+    } else if (p.B > 1) {
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             if (b0 > 0) lens = b0 + lane < p.B ? seq_keys(p, b0 + lane) : 0;
             const int nt = b0 + lane < p.B ? SeqTiles(lens, p).n_tiles : 0;

@@ -305,6 +305,9 @@ def test_attend(ctx, L, hq, hkv, d, page, lens, window, sinks):
     (32, 28, 4, 128, 64, 7, 300, 0, 0),                      # 224 rows in two tiles, one of them half full
     (32, 28, 4, 128, 16, 29, 150, 0, 0),                     # both tiles of a pair
     (32, 28, 4, 128, 32, 29, 260, 50, 3),
+    (32, 28, 4, 64, 16, 29, 700, 0, 0),                      # the long ones of them taken one tile at a time
+    (32, 28, 4, 64, 32, 29, 900, 400, 4),
+    (19, 14, 2, 64, 16, 60, 600, 0, 0),                      # 133 rows: a full tile and one of 7
     (32, 28, 4, 128, 16, 7, 700, 64, 70),
     (97, 4, 4, 64, 16, 10, 300, 0, 0),                       # one tile per sequence, 31 rows of it empty
     (130, 16, 4, 64, 128, 13, 260, 0, 0),                    # five tiles
