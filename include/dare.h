@@ -462,7 +462,7 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  *   once.  A position outside [0, n_positions) gives zeros and sets DARE_DEV_INDEX_OUTSIDE.
  * dare_qk_norm_rope_backward: given the gradients d_q, d_k, d_v of those outputs, d_qkv bf16 (shape of qkv) and, with weights,
  *   d_q_weight, d_k_weight fp32 [d] (sums over all rows and heads in a fixed order; without weights ignored).  A row that the forward
- *   left at zero has a zero gradient.  Needs ctx workspace of 16 * d * (number of SMs) bytes with weights.
+ *   left at zero has a zero gradient.  Needs ctx workspace of 8 * d * (number of SMs) bytes with weights.
  *
  * The paged cache: k_pages, v_pages bf16 [n_pages, Hkv, page_size, d]; block_table int32 [n_seqs, max_pages]: position j of
  * sequence b lives in page block_table[b, j / page_size] at index j % page_size.  Sequences may share pages.  page_size: a

@@ -31,12 +31,16 @@ constexpr float LN2_F = 0.6931471805599453f;
 constexpr int PG_KT = 64;          // keys per tile
 constexpr int PG_ROWS = 8;         // packed query rows of a unit, at most
 constexpr int PG_WARPS = 4;        // consumers, each with 16 of a tile's keys
-// Tiles that the longest unit may have more than a stretch of equal length has, and units still be taken whole: joining costs a CTA
-// 7.4 k cycles at its end, some five tiles' time (32 sequences x 8 heads of 17 or 18 tiles on 296 CTAs: 29.7 us in stretches, 25.4 whole).
-constexpr int PG_LONGER = 5;
+// Where there is a CTA for each unit, units are taken whole if the longest has no more tiles than PG_SHARES equal shares of all tiles on all
+// places and PG_LONGER more: joining costs a CTA 5 to 7.4 k cycles at its end, a tile 0.9 (few CTAs) to 1.5 k (all of them reading).  us cut
+// evenly / whole on 296 places, 28 + 4 heads: 256 units of 64 tiles 89.5 / 81.5, 148 of 47 43.8 / 39.9, 148 of 16 19.9 / 17.3, 72 of 11 11.8 / 10.6;
+// 72 of 32 19.8 / 23.3, 4 of 8 6.7 / 8.4, 4 of 125 13.7 / 71.7.
+constexpr int PG_SHARES = 2, PG_LONGER = 6;
+constexpr float PG_LEAST = 0.4f;   // see Stretches
 constexpr int PG_UNITS = 8;        // descriptors of units on their way
 
 struct PagedParams {
+    int places;                           // CTAs that the GPU holds at once
     int B, L, Hq, Hkv, g, R;              // R = L * g packed query rows per (sequence, KV head)
     int page_shift, n_pages, max_pages;
     int window, sinks;                    // window 0: all keys
@@ -101,12 +105,19 @@ struct SeqTiles {
     __device__ __forceinline__ int key0(int t) const { return (t < n_sink ? t : win_tile + t - n_sink) * PG_KT; }
 };
 
-// The list of all units' tiles cut into stretches of equal length (to one tile), one per CTA (none where there are fewer tiles).  As
-// many CTAs as that gives even where each then has one tile: a tile after another costs a CTA more than one part more costs those who
-// join them (1 sequence of 777 keys on 52, 26 and 17 CTAs 8.0, 9.7 and 10.8 us).
+// The list of all units' tiles cut into stretches of equal length (to one tile), one per CTA (none where there are fewer tiles).  A tile
+// after another costs a CTA about as much as eight parts more cost those who join them: the sum of both is least where a stretch
+// has PG_LEAST sqrt(tiles of the longest unit) tiles, so it has that many at least, unless units would have to share CTAs for it
+// (us for 1 sequence of 777, 4000, 8000 and 40000 keys, 28 + 4 heads, with 0.4: 7.8, 10.4, 13.3, 24.9; with stretches of one tile and more:
+// 7.8, 12.4, 22.0, 27.4; with 0.6: 9.5, 12.8, 13.1, 26.9).
 struct Stretches {
     int n, each, more;        // CTAs that have one; tiles of each; the first `more` have one tile more
-    __device__ __forceinline__ Stretches(int tiles, int ctas) : n(min(tiles, ctas)), each(tiles / n), more(tiles - each * n) {}
+    __device__ __forceinline__ Stretches(int tiles, int units, int longest, int ctas) {
+        const int least = max(1, static_cast<int>(PG_LEAST * sqrtf(static_cast<float>(longest))));
+        n = min(ctas, max(units, tiles / least));
+        each = tiles / n;
+        more = tiles - each * n;
+    }
     __device__ __forceinline__ int begin(int cta) const { return min(cta, n) * each + min(cta, more); }
     __device__ __forceinline__ int cta_of(int tile) const {
         const int longer = more * (each + 1);
@@ -221,10 +232,9 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             if (g0 + i == 0) lens = keys;
         }
     }
-    const Stretches st(total * p.Hkv, gridDim.x);
+    const Stretches st(total * p.Hkv, p.B * p.Hkv, longest, gridDim.x);
     int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
-    // Where there is a CTA for each unit and the longest one is not much longer than a stretch, each takes a unit: nothing to join.
-    const bool unit_each = p.B * p.Hkv <= static_cast<int>(gridDim.x) && longest <= st.each + PG_LONGER;
+    const bool unit_each = p.B * p.Hkv <= static_cast<int>(gridDim.x) && longest - PG_LONGER <= PG_SHARES * total * p.Hkv / p.places;
     if (unit_each) begin = 0, end = static_cast<int>(blockIdx.x) < p.B * p.Hkv;
     if (begin >= end) {
         if (lane == 0) {
@@ -668,9 +678,10 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     a.scale = scale != 0.f ? scale : 1.0f / sqrtf(static_cast<float>(d));
     a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.table = block_table; a.kv_lens = kv_lens; a.out = out; a.lse = lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // Up to PG_ROWS packed query rows take the kernel of this file, more the tcgen05 kernel.  us here / there: 7 rows, 1 sequence of 8000
-    // keys 16.4 / 16.9, 18 of 2000 19.5 / 21.3, 74 of 1000 29.1 / 32.5.  With the rows as the MMA's 16 rows instead of its 8 columns, 9
-    // to 16 rows took 25.6 / 17.3, 22.4 / 21.3 and 31.4 / 32.7, and 32 rows 46 / 17.5, 38 / 21.6 and 39.5 / 33.4.
+    // Up to PG_ROWS packed query rows take the kernel of this file, more the tcgen05 kernel.  us here / there: 7 rows, 1 sequence of 300 keys
+    // 6.8 / 9.2, of 8000 13.3 / 16.6, 18 of 2000 20.0 / 21.2, 64 of 4096 82 / 95, 74 of 250 to 4000 62 / 82.  With the rows as the MMA's 16 rows
+    // instead of its 8 columns, 9 to 16 rows took 25.6 / 17.3, 22.4 / 21.3 and 31.4 / 32.7 for 1 of 8000, 18 of 2000 and 74 of 1000, and 32 rows
+    // 46 / 17.5, 38 / 21.6 and 39.5 / 33.4.
     if (L * (Hq / Hkv) > PG_ROWS) {
         if (static_cast<long long>(B) * Hkv > 65535) return DARE_ERR_SHAPE;      // (a grid's second dimension)
         return launch_attn_paged_tc(ctx, a, s);
@@ -686,9 +697,10 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     p.counters = ctx->join_counters; p.dev_status = ctx->dev_status;
     // two CTAs per SM, all resident at once; no more than there can be tiles
     const long long tiles = static_cast<long long>(B) * Hkv * ((static_cast<long long>(max_pages) * page_size + PG_KT - 1) / PG_KT);
-    if (tiles > (1LL << 30)) return DARE_ERR_SHAPE;
+    if (tiles > (1LL << 29)) return DARE_ERR_SHAPE;
     long long ctas = 2LL * ctx->sm_count;
     if (ctas > PAGED_MAX_CTAS) ctas = PAGED_MAX_CTAS;
+    p.places = static_cast<int>(ctas);
     if (ctas > tiles) ctas = tiles;
     const size_t part_rows = static_cast<size_t>(ctas) * 2 * PG_ROWS;
     if (part_rows * (d + 2) * sizeof(float) > ctx->workspace_bytes) return DARE_ERR_WORKSPACE;

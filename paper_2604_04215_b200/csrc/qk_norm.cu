@@ -23,7 +23,7 @@ namespace {
 enum { QKN_DENSE = 0, QKN_APPEND = 1, QKN_BACKWARD = 2 };
 
 // One CTA per SM.  Stages of an item's run of heads, in the backward pass of values and of gradients: one that is worked on, the next one,
-// one on its way out.  As fast as a plain copy of the same bytes is here (4310 rows of 32 + 32 + 32 heads of 128 36.6 us, copied 36.7;
+// one on its way out.  As fast as a plain copy of the same bytes is here (3798 rows of 32 + 32 + 32 heads of 128 36.6 us, copied 36.7;
 // 19201 of 28 + 4 + 4 57 to 61, copied 61.4); 12 and 14 warps with larger stages 60 to 66 there.  The backward pass spills with 16 warps'
 // 128 registers: 151 us instead of 88.
 template <int MODE>
@@ -343,7 +343,7 @@ qk_norm_kernel(const QkNormParams p) {
             if (lane == 0 && it.nq) bulk_store(p.q_out + (static_cast<int64_t>(it.row) * p.Hq + it.q0) * D, at, it.nq * HEAD);
             at += it.nq * HEAD;
             if (APPEND) {
-                // A head's place is a row of its page: short for bulk copies (one each cost 37.8 us instead of 36.8 at 7473 rows of 32 + 32 + 32 heads
+                // A head's place is a row of its page: short for bulk copies (one each cost 37.8 us instead of 36.8 at 3798 rows of 32 + 32 + 32 heads
                 // of 128).
                 const int64_t in_page = pos & ((1 << p.page_shift) - 1);
                 for (int o = lane; o < (it.nk + it.nv) * (D / 8); o += 32) {
