@@ -23,8 +23,8 @@ namespace {
 enum { QKN_DENSE = 0, QKN_APPEND = 1, QKN_BACKWARD = 2 };
 
 // One CTA per SM.  Stages of an item's run of heads, in the backward pass of values and of gradients: one that is worked on, the next one,
-// one on its way out.  As fast as a plain copy of the same bytes is here (3798 rows of 32 + 32 + 32 heads of 128 36.6 us, copied 36.7;
-// 19201 of 28 + 4 + 4 57 to 61, copied 61.4); 12 and 14 warps with larger stages 60 to 66 there.  The backward pass spills with 16 warps'
+// one on its way out.  About as fast as a plain copy of the same bytes (4310 rows of 32 + 32 + 32 heads of 128 dense 36.7 us, copied 35.1 to
+// 36.7; 19201 of 28 + 4 + 4 57 to 60, copied 61); 12 and 14 warps with larger stages 60 to 66 there.  The backward pass spills with 16 warps'
 // 128 registers: 151 us instead of 88.
 template <int MODE>
 struct QkNormShape {
@@ -246,13 +246,13 @@ qk_norm_kernel(const QkNormParams p) {
     }
     const uint4 *wq = normed ? weights[0] : nullptr, *wk = normed ? weights[1] : nullptr;
 
-    auto send_for = [&](const ItemWalk& w, int stage) {                      // lane 0
+    auto send_for = [&](const ItemWalk& w, int stage, bool wanted) {         // lane 0; an item that is not wanted arrives without bytes
         const Item it(w.row, w.k, p.item_heads, p.Hq, p.Hkv);
         uint8_t* dst = ring + stage * QKN_STAGE_BYTES;
         uint64_t* bar = &bars[warp][stage];
         const uint32_t all = static_cast<uint32_t>(it.nq + it.nk + it.nv) * HEAD;
         // (the backward pass reads the values of queries and keys, where they are normalised)
-        const uint32_t values = !BACK ? all : normed ? static_cast<uint32_t>(it.nq + it.nk) * HEAD : 0;
+        const uint32_t values = !wanted ? 0 : !BACK ? all : normed ? static_cast<uint32_t>(it.nq + it.nk) * HEAD : 0;
         mbar_arrive_expect_tx(bar, values + (BACK ? all : 0));
         if (values) bulk_load(dst, p.qkv + (static_cast<int64_t>(it.row) * heads_in + it.h0) * D, values, bar);
         if (BACK) {
@@ -266,10 +266,10 @@ qk_norm_kernel(const QkNormParams p) {
     uint64_t acc[2][8];                                                      // the weights' gradients, pairs of channels
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[0][j] = acc[1][j] = 0;
-    if (lane == 0 && ahead.row < p.rows) send_for(ahead, 0);
+    if (lane == 0 && ahead.row < p.rows) send_for(ahead, 0, true);
     ahead.next();
     // What an item needs besides its heads is asked for ahead of it, so that nothing waits for it: its position (and sequence) two
-    // items before, its angles (and page) one item before.  (In the backward pass the angles that wait would spill: 106 us instead of 95.)
+    // items before, its angles (and page) one item before.  (In the backward pass the angles that wait would spill: 106 us instead of 95 at 19201 rows.)
     struct Place { int pos, seq; };
     auto place_of = [&](const ItemWalk& w) -> Place {
         return w.row < p.rows ? Place{p.positions[w.row], APPEND ? p.seq_ids[w.row] : 0} : Place{-1, -1};
@@ -310,7 +310,8 @@ qk_norm_kernel(const QkNormParams p) {
         // the next item takes the place of the last but one, once the copies out of that have read it
         bulk_wait_read<1>();
         __syncwarp();
-        if (lane == 0 && ahead.row < p.rows) send_for(ahead, stage == QKN_STAGES - 1 ? 0 : stage + 1);
+        // (append: rows of no sequence, as in a padded batch, are not read: 34.1 us instead of 36.5 where 512 of 4310 are)
+        if (lane == 0 && ahead.row < p.rows) send_for(ahead, stage == QKN_STAGES - 1 ? 0 : stage + 1, !APPEND || place1.seq >= 0);
         ahead.next();
         uint64_t cs[4], sn[4];
 #pragma unroll
@@ -343,8 +344,8 @@ qk_norm_kernel(const QkNormParams p) {
             if (lane == 0 && it.nq) bulk_store(p.q_out + (static_cast<int64_t>(it.row) * p.Hq + it.q0) * D, at, it.nq * HEAD);
             at += it.nq * HEAD;
             if (APPEND) {
-                // A head's place is a row of its page: short for bulk copies (one each cost 37.8 us instead of 36.8 at 3798 rows of 32 + 32 + 32 heads
-                // of 128).
+                // A head's place is a row of its page: short for bulk copies (one each cost 37.8 us instead of 36.8 at 4310 rows of 32 + 32 + 32 heads
+                // of 128, 512 of them of no sequence).
                 const int64_t in_page = pos & ((1 << p.page_shift) - 1);
                 for (int o = lane; o < (it.nk + it.nv) * (D / 8); o += 32) {
                     const int h = o / (D / 8);
