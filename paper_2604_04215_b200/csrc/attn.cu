@@ -1106,7 +1106,7 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             dst[c * 8 + k] = make_float4(__uint_as_float(ov[4 * k]) * inv, __uint_as_float(ov[4 * k + 1]) * inv,
                                                          __uint_as_float(ov[4 * k + 2]) * inv, __uint_as_float(ov[4 * k + 3]) * inv);
                 }
-                if (live) p.part_lse[w.split * n_rows + row] = l > 0.f ? (m_ref + log2f(l)) * LN2_F : -INFINITY;
+                if (live) p.part_lse[w.split * n_rows + row] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * LN2_F;      // (a NaN stays one)
                 __syncwarp();
                 tc_fence_before_sync();
                 continue;
@@ -1146,7 +1146,7 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (p.lse != nullptr && r < rows_in_tile && pos0 + ri < w.L_eff) {
                 const int i = pos0 + ri, h = w.kvh * p.g + rh;
                 p.lse[packed ? static_cast<size_t>(h) * p.total_tokens + w.token0 + i
-                             : (static_cast<size_t>(w.b) * p.Hq + h) * p.L + i] = l > 0.f ? (m_ref + log2f(l)) * LN2_F : -INFINITY;
+                             : (static_cast<size_t>(w.b) * p.Hq + h) * p.L + i] = (PAGED ? l != 0.f : l > 0.f) ? (m_ref + log2f(l)) * LN2_F : -INFINITY;
             }
         }
     }
@@ -1216,7 +1216,7 @@ __global__ void attn_combine_kernel(const float* __restrict__ part_o, const floa
     if (lse != nullptr && c4 == 0) {
         // row = (b * L + i) * Hq + h  ->  lse[b, h, i]
         const size_t h = row % Hq, bi = row / Hq, i = bi % L, bb = bi / L;
-        lse[(bb * Hq + h) * L + i] = wsum > 0.f ? mx + logf(wsum) : -INFINITY;
+        lse[(bb * Hq + h) * L + i] = wsum == 0.f ? -INFINITY : mx + logf(wsum);
     }
 }
 

@@ -130,7 +130,7 @@ __device__ __forceinline__ int seq_keys(const PagedParams& p, int b) {
 }
 
 __device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }      // (a NaN stays one)
-__device__ __forceinline__ float log_sum(float m, float l) { return m == -INFINITY ? -INFINITY : (m + log2f(l)) * LN2_F; }
+__device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l)) * LN2_F; }      // (nothing visible: -inf)
 
 // Adds a unit's parts up, in the order of the keys (the order of arrival does not show).  A thread has four channels of a row,
 // two rows at once, and asks for JOIN parts at a time: what this costs is trips to L2, one after the other.

@@ -387,6 +387,26 @@ def test_attend_large_scores(ctx):
     _check_attend(out, lse, q, kp, vp, table, lens, 0, 0)
 
 
+@pytest.mark.parametrize("B,L,hq,hkv,n", [(2, 1, 14, 2, 300), (1, 1, 28, 4, 8000), (2, 32, 28, 4, 500), (1, 16, 14, 2, 4000), (9, 200, 28, 4, 600)])
+def test_attend_query_that_is_not_finite(ctx, B, L, hq, hkv, n):
+    """NaN in that query's own output and log-sum, nothing elsewhere: units whole and in parts, both kernels."""
+    d, page, per = 128, 64, -(-n // 64)
+    k, v = (I.normal_bf16(B + n, t, (B * per, hkv, page, d)).cuda() for t in (1, 2))
+    q = I.normal_bf16(B + n, 3, (B, L, hq, d)).cuda()
+    table = torch.arange(B * per, dtype=torch.int32, device="cuda").view(B, per)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    lse, lse0 = (torch.empty(B, hq, L, device="cuda") for _ in range(2))
+    out0 = dare.dare_attn_paged(ctx, q, k, v, table, lens, lse=lse0)
+    for value in (float("nan"), float("inf")):
+        bad = q.clone()
+        bad[0, L // 2, 1, 3] = value
+        out = dare.dare_attn_paged(ctx, bad, k, v, table, lens, lse=lse)
+        assert out[0, L // 2, 1].isnan().all() and lse[0, 1, L // 2].isnan()
+        out[0, L // 2, 1], lse[0, 1, L // 2] = out0[0, L // 2, 1], lse0[0, 1, L // 2]
+        assert torch.equal(out, out0) and torch.equal(lse, lse0)
+    assert ctx.device_status() == 0
+
+
 def test_attend_reports_lengths_and_pages_outside(ctx):
     lens = [200, 100]
     q, kp, vp, table = _attend_case(3, 2, 1, 4, 2, 64, 16, lens, 0, 0, plant=False)
