@@ -481,7 +481,7 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  *   (DARE_DEV_LEN_CLAMPED).  Pages that no query of the block can see, those between the sinks and the window and those
  *   behind n, are not read and their table entries may be anything; a page outside [0, n_pages) that one can see reads as zeros and
  *   sets DARE_DEV_INDEX_OUTSIDE.  Cached values that some query of a block sees must be finite for all of its queries.
- *   A query that is not finite has NaN in its own out and lse and nowhere else.  Results do not depend on the order in which the GPU
+ *   A query that is not finite has NaN in its own out and lse (where n > 0) and nowhere else.  Results do not depend on the order in which the GPU
  *   runs the parts.  Supported: Hq % Hkv == 0, Hq / Hkv <= 128, d in {64, 128}, L >= 1, L * Hq / Hkv <= 2^20, B * Hkv <= 65535 where
  *   that is more than 8; ctx workspace of 128 * (d + 2) bytes for each SM.
  *   n may be smaller than L (the positions of the first queries are then negative, the rule of what is visible stays).

@@ -1084,7 +1084,9 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (ok) ok = mbar_wait(&bars->pv_done[j][(n_s - 1) & 1], ((n_s - 1) >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after_sync();
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            // (PAGED: where there are keys, key n - 1 is visible to every query; a row of a whole unit whose sum is 0 has scores of -inf alone, as
+            // with an infinity in the query: 0 / 0.  A part's keys may all be hidden: attn_combine_kernel leaves it out.)
+            const float inv = l > 0.f ? 1.f / l : PAGED && w.len_pre > 0 ? NAN : 0.f;
             // O rows leave through shared memory so that the global stores are coalesced (a thread holds one whole row,
             // and 32 lanes storing 16 bytes each to 32 different rows cost a request per lane): 64 columns at a time,
             // 16-byte chunk c of row r at c ^ (r & 7).
@@ -1146,7 +1148,7 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (p.lse != nullptr && r < rows_in_tile && pos0 + ri < w.L_eff) {
                 const int i = pos0 + ri, h = w.kvh * p.g + rh;
                 p.lse[packed ? static_cast<size_t>(h) * p.total_tokens + w.token0 + i
-                             : (static_cast<size_t>(w.b) * p.Hq + h) * p.L + i] = (PAGED ? l != 0.f : l > 0.f) ? (m_ref + log2f(l)) * LN2_F : -INFINITY;
+                             : (static_cast<size_t>(w.b) * p.Hq + h) * p.L + i] = l > 0.f ? (m_ref + log2f(l)) * LN2_F : PAGED && w.len_pre > 0 ? NAN : -INFINITY;
             }
         }
     }
@@ -1186,11 +1188,12 @@ bool use_tc_path(const AttnArgs& a) {
     return rows >= 96;
 }
 
-// Combine KV-split partials: out = sum_s w_s o_s / sum_s w_s with w_s = exp(lse_s - max lse).
+// Combine KV-split partials: out = sum_s w_s o_s / sum_s w_s with w_s = exp(lse_s - max lse).  kv_lens (paged keys, else NULL): a row
+// without any weight of a sequence that has keys is NaN (see the parts).
 template <int D>
 __global__ void attn_combine_kernel(const float* __restrict__ part_o, const float* __restrict__ part_lse, int splits,
-                                    size_t n_rows, int L, int Hq, __nv_bfloat16* __restrict__ out,
-                                    float* __restrict__ lse) {
+                                    size_t n_rows, int L, int Hq, const int32_t* __restrict__ kv_lens,
+                                    __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     const size_t row = static_cast<size_t>(blockIdx.x) * (blockDim.x / (D / 4)) + threadIdx.x / (D / 4);
     const int c4 = threadIdx.x % (D / 4);
     pdl_wait();
@@ -1208,7 +1211,8 @@ __global__ void attn_combine_kernel(const float* __restrict__ part_o, const floa
         acc.x += w * o.x; acc.y += w * o.y; acc.z += w * o.z; acc.w += w * o.w;
         wsum += w;
     }
-    const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
+    const bool no_weight = wsum == 0.f && kv_lens != nullptr && kv_lens[row / Hq / L] > 0;
+    const float inv = wsum > 0.f ? 1.f / wsum : no_weight ? NAN : 0.f;
     uint2 packed;
     packed.x = pack_bf16(acc.x * inv, acc.y * inv);
     packed.y = pack_bf16(acc.z * inv, acc.w * inv);
@@ -1216,7 +1220,7 @@ __global__ void attn_combine_kernel(const float* __restrict__ part_o, const floa
     if (lse != nullptr && c4 == 0) {
         // row = (b * L + i) * Hq + h  ->  lse[b, h, i]
         const size_t h = row % Hq, bi = row / Hq, i = bi % L, bb = bi / L;
-        lse[(bb * Hq + h) * L + i] = wsum == 0.f ? -INFINITY : mx + logf(wsum);
+        lse[(bb * Hq + h) * L + i] = no_weight ? NAN : wsum == 0.f ? -INFINITY : mx + logf(wsum);
     }
 }
 
@@ -1225,7 +1229,7 @@ int launch_combine(const AttnParams& p, size_t n_rows, int d, cudaStream_t strea
     const int rows_per_block = 256 / tpr;
     const unsigned blocks = static_cast<unsigned>((n_rows + rows_per_block - 1) / rows_per_block);
     return launch_kernel(d == 128 ? attn_combine_kernel<128> : attn_combine_kernel<64>, dim3(blocks), 256, 0, stream, 1,
-                         p.part_o, p.part_lse, p.splits, n_rows, p.L, p.Hq, p.out, p.lse);
+                         p.part_o, p.part_lse, p.splits, n_rows, p.L, p.Hq, p.kv_lens, p.out, p.lse);
 }
 
 template <int D, int NW, int KS, int KT, int STAGES, int CPS>

@@ -129,8 +129,11 @@ __device__ __forceinline__ int seq_keys(const PagedParams& p, int b) {
     return max(0, min(p.kv_lens[b], p.max_pages << p.page_shift));
 }
 
-__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }      // (a NaN stays one)
-__device__ __forceinline__ float log_sum(float m, float l) { return (m + log2f(l)) * LN2_F; }      // (nothing visible: -inf)
+// What a row of a sequence of n keys is divided by, and its lse.  Key n - 1 is visible to every query, and a row's largest score has
+// weight 1: a sum of 0 is that of a sequence without keys, or of a row whose visible scores are all -inf, as with an infinity in the
+// query that meets keys of the other sign (0 / 0: NaN, as with a NaN in the query).
+__device__ __forceinline__ float inverse_sum(float l, int n) { return l > 0.f ? 1.f / l : n > 0 ? NAN : 0.f; }
+__device__ __forceinline__ float log_sum(float m, float l, int n) { return l > 0.f ? (m + log2f(l)) * LN2_F : n > 0 ? NAN : -INFINITY; }
 
 // Adds a unit's parts up, in the order of the keys (the order of arrival does not show).  A thread has four channels of a row,
 // two rows at once, and asks for JOIN parts at a time: what this costs is trips to L2, one after the other.
@@ -182,12 +185,12 @@ __device__ __forceinline__ void join_parts(const PagedParams& p, const UnitDesc&
         for (int e = 0; e < 2; ++e) {
             const int item = item0 + e * THREADS;
             if (item >= items) continue;
-            const float inv = inverse_sum(l[e]);
+            const float inv = inverse_sum(l[e], u.n);
             const int rho = item / (D / 4), c4 = item % (D / 4), i = rho / p.g, h = u.kvh * p.g + rho - i * p.g;
             *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(u.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
                 make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
             if (p.lse != nullptr && c4 == 0)
-                p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(m[e], l[e]);
+                p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(m[e], l[e], u.n);
         }
     }
 }
@@ -532,11 +535,11 @@ struct FewRows {
                 acc.x += x.x * w; acc.y += x.y * w; acc.z += x.z * w; acc.w += x.w * w;
             }
             if (whole) {
-                const float inv = inverse_sum(sum);
+                const float inv = inverse_sum(sum, u.n);
                 const int i = p.L == 1 ? 0 : q / p.g, h = u.kvh * p.g + q - i * p.g;
                 *reinterpret_cast<uint2*>(p.out + ((static_cast<size_t>(u.b) * p.L + i) * p.Hq + h) * D + c4 * 4) =
                     make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                if (p.lse != nullptr && c4 == 0) p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(top, sum);
+                if (p.lse != nullptr && c4 == 0) p.lse[(static_cast<size_t>(u.b) * p.Hq + h) * p.L + i] = log_sum(top, sum, u.n);
             } else {
                 *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(u.slot) * PG_ROWS + q) * D + c4 * 4) = acc;
                 if (c4 == 0) reinterpret_cast<float2*>(p.part_ml)[u.slot * PG_ROWS + q] = make_float2(top, sum);

@@ -407,6 +407,38 @@ def test_attend_query_that_is_not_finite(ctx, B, L, hq, hkv, n):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("B,L,hq,hkv,n,window", [
+    (2, 1, 14, 2, 1, 0), (3, 4, 4, 2, 2, 0), (2, 1, 14, 2, 300, 0), (1, 1, 28, 4, 8000, 0), (1, 1, 28, 4, 8000, 3000),      # up to 8 rows
+    (2, 32, 28, 4, 1, 0), (9, 200, 28, 4, 600, 0), (2, 32, 28, 4, 500, 0), (1, 16, 14, 2, 4000, 0), (1, 16, 14, 2, 4000, 1500)])
+def test_attend_query_whose_scores_are_all_minus_infinity(ctx, B, L, hq, hkv, n, window):
+    """An infinite channel whose product with every visible key has the same sign: NaN for either sign, in units whole and in parts; a batch place
+    without keys stays zero and -inf whatever its queries are."""
+    d, page, per = 128, 64, -(-n // 64)
+    k, v = (I.normal_bf16(B + n, t, (B * per, hkv, page, d)).cuda() for t in (1, 2))
+    k[..., 3] = k[..., 3].abs() + 0.5
+    q = I.normal_bf16(B + n, 3, (B, L, hq, d)).cuda()
+    table = torch.arange(B * per, dtype=torch.int32, device="cuda").view(B, per)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    if B > 1:
+        lens[B - 1] = 0
+    lse, lse0 = (torch.empty(B, hq, L, device="cuda") for _ in range(2))
+    out0 = dare.dare_attn_paged(ctx, q, k, v, table, lens, window=window, lse=lse0)
+    assert out0.isfinite().all()
+    for value in (float("inf"), -float("inf")):
+        bad = q.clone()
+        bad[0, L // 2, 1, 3] = value
+        if B > 1:
+            bad[B - 1, 0, :, 3] = value
+        out = dare.dare_attn_paged(ctx, bad, k, v, table, lens, window=window, lse=lse)
+        assert out[0, L // 2, 1].isnan().all() and lse[0, 1, L // 2].isnan()
+        out[0, L // 2, 1], lse[0, 1, L // 2] = out0[0, L // 2, 1], lse0[0, 1, L // 2]
+        if window:                                           # (a row may move its warp's reference a tile later: other roundings)
+            assert out.isfinite().all() and lse.isfinite().all()
+        else:
+            assert torch.equal(out, out0) and torch.equal(lse, lse0)
+    assert ctx.device_status() == 0
+
+
 def test_attend_reports_lengths_and_pages_outside(ctx):
     lens = [200, 100]
     q, kp, vp, table = _attend_case(3, 2, 1, 4, 2, 64, 16, lens, 0, 0, plant=False)
