@@ -454,14 +454,18 @@ struct FewRows {
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
             t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
             mn[e] = fmaxf(m[e], t);
-            r[e] = mn[e] == -INFINITY ? 0.f : mn[e] * c;      // (a row may have seen nothing yet: weights exp2(-inf) = 0)
+            r[e] = mn[e] == -INFINITY ? 0.f : __fmul_rn(mn[e], c);      // (a row may have seen nothing yet: weights exp2(-inf) = 0)
             same = same && mn[e] == m[e];
         }
         float w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = fast_exp2(fmaf(s[e], c, -r[e & 1]));
         if (__any_sync(0xffffffffu, !same)) {
-            const float f0 = fast_exp2(fmaf(m[0], c, -r[0])), f1 = fast_exp2(fmaf(m[1], c, -r[1]));
+            // From the old reference, rounded as it was when weights were taken against it, to the new one: exactly 1 for a row that stays.
+            // (The unrounded product is up to 2^-24 of itself away from it, each time that another row's maximum moves; a row
+            // without a maximum has nothing to carry over.)
+            const float f0 = m[0] == -INFINITY ? 0.f : fast_exp2(__fmul_rn(m[0], c) - r[0]);
+            const float f1 = m[1] == -INFINITY ? 0.f : fast_exp2(__fmul_rn(m[1], c) - r[1]);
             m[0] = mn[0];
             m[1] = mn[1];
             l[0] *= f0;
@@ -506,7 +510,7 @@ struct FewRows {
             l[e] += __shfl_xor_sync(0xffffffffu, l[e], 4);
             l[e] += __shfl_xor_sync(0xffffffffu, l[e], 8);
             l[e] += __shfl_xor_sync(0xffffffffu, l[e], 16);
-            if (quad == 0) ml[ks * 8 + 2 * tq + e] = make_float2(m[e] * p.scale_log2, l[e]);
+            if (quad == 0) ml[ks * 8 + 2 * tq + e] = make_float2(__fmul_rn(m[e], p.scale_log2), l[e]);
             float* x = at(ks, 2 * tq + e);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {

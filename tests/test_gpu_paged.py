@@ -439,6 +439,36 @@ def test_attend_query_whose_scores_are_all_minus_infinity(ctx, B, L, hq, hkv, n,
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("n,per_sm", [(64 * 600, 2), (64 * 40, 2), (64 * 3000, 1)])
+def test_attend_a_rows_sum_does_not_move_with_its_neighbours_maximum(ctx, n, per_sm):
+    """Two heads on the same keys, a unit per CTA.  All scores of the first are equal, 4126.5 scale, which has no 24-bit logarithm to the base 2; those of the second
+    rise with every tile, so that its maximum moves each time.  With values 1 over the first half of the keys and 0 over the second
+    the first head's output is 1/2, and what the second one does must not show in it."""
+    d, page, tiles = 64, 64, n // 64
+    B = per_sm * torch.cuda.get_device_properties(0).multi_processor_count
+    t = torch.arange(tiles, dtype=torch.float32)
+    k, v = (torch.zeros(tiles, 1, page, d) for _ in range(2))
+    k[..., 0] = 63.0
+    k[..., 1], k[..., 2], k[..., 3] = ((t // 256).view(-1, 1, 1), (t // 16 % 16).view(-1, 1, 1), (t % 16).view(-1, 1, 1))
+    v[:tiles // 2, ..., 0] = 1.0
+    k, v = (x.to(torch.bfloat16).cuda() for x in (k, v))
+    table = torch.arange(tiles, dtype=torch.int32, device="cuda").repeat(B, 1)      # (all sequences share their pages)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    q = torch.zeros(B, 1, 2, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0, 0] = 65.5
+    lse, found = torch.empty(B, 2, 1, device="cuda"), []
+    for rise in (0.0, 1.0):
+        q[..., 1, 1], q[..., 1, 2], q[..., 1, 3] = 256 * rise, 16 * rise, rise
+        out = dare.dare_attn_paged(ctx, q, k, v, table, lens, lse=lse)
+        assert (out[:, 0, 0, 0] == 0.5).all()
+        found.append(lse[:, 0].clone())
+    assert torch.equal(*found)
+    # an fp32 sum of n / 4 equal weights a warp at most, pairs of them at a time; the logarithms' and the product's rounding
+    want = 65.5 * 63.0 * 0.125 + np.log(n)
+    assert np.abs(found[0].double().cpu().numpy() - want).max() <= 2.0 ** -21 * (want + 1) + n / 32 * 2.0 ** -24
+    assert ctx.device_status() == 0
+
+
 def test_attend_reports_lengths_and_pages_outside(ctx):
     lens = [200, 100]
     q, kp, vp, table = _attend_case(3, 2, 1, 4, 2, 64, 16, lens, 0, 0, plant=False)
