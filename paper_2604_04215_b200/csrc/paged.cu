@@ -110,18 +110,21 @@ struct SeqTiles {
 // has PG_LEAST sqrt(tiles of the longest unit) tiles, so it has that many at least, unless units would have to share CTAs for it
 // (us for 1 sequence of 777, 4000, 8000 and 40000 keys, 28 + 4 heads, with 0.4: 7.8, 10.4, 13.3, 24.9; with stretches of one tile and more:
 // 7.8, 12.4, 22.0, 27.4; with 0.6: 9.5, 12.8, 13.1, 26.9).
+// T numbers the list's tiles (see dare_attn_paged).
+template <typename T>
 struct Stretches {
-    int n, each, more;        // CTAs that have one; tiles of each; the first `more` have one tile more
-    __device__ __forceinline__ Stretches(int tiles, int units, int longest, int ctas) {
+    int n;                    // CTAs that have one
+    T each, more;             // tiles of each; the first `more` have one tile more
+    __device__ __forceinline__ Stretches(T tiles, int units, int longest, int ctas) {
         const int least = max(1, static_cast<int>(PG_LEAST * sqrtf(static_cast<float>(longest))));
-        n = min(ctas, max(units, tiles / least));
+        n = static_cast<int>(min(static_cast<T>(ctas), max(static_cast<T>(units), tiles / least)));
         each = tiles / n;
         more = tiles - each * n;
     }
-    __device__ __forceinline__ int begin(int cta) const { return min(cta, n) * each + min(cta, more); }
-    __device__ __forceinline__ int cta_of(int tile) const {
-        const int longer = more * (each + 1);
-        return tile < longer ? tile / (each + 1) : more + (tile - longer) / each;
+    __device__ __forceinline__ T begin(int cta) const { return min(cta, n) * each + min(static_cast<T>(cta), more); }
+    __device__ __forceinline__ int cta_of(T tile) const {
+        const T longer = more * (each + 1);
+        return static_cast<int>(tile < longer ? tile / (each + 1) : more + (tile - longer) / each);
     }
 };
 
@@ -212,14 +215,15 @@ struct PagedSmem {
 
 // The producer warp: finds this CTA's stretch of the list of tiles (sequence by sequence, in it KV head by KV head) and sends for
 // its tiles.
-template <int D>
+template <int D, typename T>
 __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorMap* tm_v, const PagedParams& p, const PagedSmem<D>& sm) {
     using S = PagedShape<D>;
     constexpr int STAGES = S::STAGES, KV_BYTES = PG_KT * D * 2;
     PagedBarriers<STAGES>* bars = sm.bars;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int lane = threadIdx.x & 31;
-    int total = 0, longest = 0, lens = 0;          // (lens, lane i: keys of sequence (b & ~31) + i)
+    T total = 0;
+    int longest = 0, lens = 0;                     // (lens, lane i: keys of sequence (b & ~31) + i)
     for (int g0 = 0; g0 < p.B; g0 += 4 * 32) {     // (four loads at a time)
         int raw[4];
 #pragma unroll
@@ -235,8 +239,8 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
             if (g0 + i == 0) lens = keys;
         }
     }
-    const Stretches st(total * p.Hkv, p.B * p.Hkv, longest, gridDim.x);
-    int begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
+    const Stretches<T> st(total * p.Hkv, p.B * p.Hkv, longest, gridDim.x);
+    T begin = st.begin(blockIdx.x), end = st.begin(blockIdx.x + 1);
     const bool unit_each = p.B * p.Hkv <= static_cast<int>(gridDim.x) && longest - PG_LONGER <= PG_SHARES * total * p.Hkv / p.places;
     if (unit_each) begin = 0, end = static_cast<int>(blockIdx.x) < p.B * p.Hkv;
     if (begin >= end) {
@@ -246,7 +250,8 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         }
         return;
     }
-    int b = 0, base = 0;                           // the sequence of tile `begin`; its first tile
+    int b = 0;                                     // the sequence of tile `begin`; its first tile
+    T base = 0;
     if (unit_each) {
         b = static_cast<int>(blockIdx.x) / p.Hkv;
         if (b >= 32) lens = (b & ~31) + lane < p.B ? seq_keys(p, (b & ~31) + lane) : 0;
@@ -260,14 +265,14 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
                 const int o = __shfl_up_sync(0xffffffffu, incl, off);
                 if (lane >= off) incl += o;
             }
-            const unsigned beyond = __ballot_sync(0xffffffffu, base + incl * p.Hkv > begin);
+            const unsigned beyond = __ballot_sync(0xffffffffu, base + static_cast<T>(incl) * p.Hkv > begin);
             if (beyond) {
                 const int i = __ffs(beyond) - 1;
                 b = b0 + i;
-                base += __shfl_sync(0xffffffffu, incl - nt, i) * p.Hkv;
+                base += static_cast<T>(__shfl_sync(0xffffffffu, incl - nt, i)) * p.Hkv;
                 break;
             }
-            base += __shfl_sync(0xffffffffu, incl, 31) * p.Hkv;
+            base += static_cast<T>(__shfl_sync(0xffffffffu, incl, 31)) * p.Hkv;
         }
     }
     // this lane's piece of a tile: rows [piece * rows_pp, + rows_pp) of K or V.  (Both halves of the columns in one copy: a copy takes
@@ -281,15 +286,15 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
     int n = __shfl_sync(0xffffffffu, lens, b & 31), kvh, t;
     {
         const int nt = SeqTiles(n, p).n_tiles;
-        kvh = unit_each ? static_cast<int>(blockIdx.x) - b * p.Hkv : (begin - base) / nt;
-        t = unit_each ? 0 : begin - base - kvh * nt;
+        kvh = unit_each ? static_cast<int>(blockIdx.x) - b * p.Hkv : static_cast<int>((begin - base) / nt);
+        t = unit_each ? 0 : static_cast<int>(begin - base - static_cast<T>(kvh) * nt);
         if (unit_each) end = nt;
     }
     int stage = 0, unit = 0;
     uint32_t phase = 0;
-    for (int at = begin; at < end;) {              // unit by unit
+    for (T at = begin; at < end;) {                // unit by unit
         const SeqTiles sq(n, p);
-        const int count = min(sq.n_tiles - t, end - at);
+        const int count = static_cast<int>(min(static_cast<T>(sq.n_tiles - t), end - at));
         // Table entries 32 pieces at a time, a lane each, the next 32 while these are on their way: the pool row that a piece is read from
         // (that behind the pool, zeros, for one that nobody may see and for one without a page).
         const int32_t* table = p.table + static_cast<long long>(b) * p.max_pages;
@@ -311,7 +316,7 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         int page = 0, page_next = 0;
         bool seen = ask(lane, page), seen_next = ask(lane + 32, page_next);
         const bool whole = t == 0 && count == sq.n_tiles;
-        const int unit0 = base + kvh * sq.n_tiles;
+        const T unit0 = base + static_cast<T>(kvh) * sq.n_tiles;
         int rows = row_of(lane, page, seen);
         bool ok = true;
         for (int i = 0; i < count; ++i) {
@@ -352,7 +357,7 @@ __device__ __forceinline__ void produce(const CUtensorMap* tm_k, const CUtensorM
         unit = (unit + 1) % PG_UNITS;
         if (++kvh == p.Hkv) {
             kvh = 0;
-            base += sq.n_tiles * p.Hkv;
+            base += static_cast<T>(sq.n_tiles) * p.Hkv;
             ++b;
             if ((b & 31) == 0) lens = b + lane < p.B ? seq_keys(p, b + lane) : 0;
             n = __shfl_sync(0xffffffffu, lens, b & 31);
@@ -553,7 +558,7 @@ struct FewRows {
     }
 };
 
-template <int D>
+template <int D, typename T>
 __global__ void __launch_bounds__((PG_WARPS + 1) * 32, 2)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
     using S = PagedShape<D>;
@@ -582,7 +587,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     pdl_wait();
 
     if (warp == NCW) {
-        produce<D>(&tm_k, &tm_v, p, sm);
+        produce<D, T>(&tm_k, &tm_v, p, sm);
     } else {
         FewRows<D> c(p);
         UnitDesc u = {};
@@ -651,13 +656,13 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
 }
 
-template <int D>
+template <int D, typename T>
 int launch_paged(const dare_ctx* ctx, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const PagedParams& p, int ctas, cudaStream_t stream) {
     using S = PagedShape<D>;
     static_assert(2 * (S::SMEM + 1024) <= 228 * 1024, "two CTAs per SM");
     static std::atomic<uint64_t> smem_set{0};
-    if (ensure_dynamic_smem(smem_set, attn_paged_kernel<D>, S::SMEM) != DARE_OK) return DARE_ERR_CUDA;
-    return launch_kernel(attn_paged_kernel<D>, dim3(ctas), (PG_WARPS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
+    if (ensure_dynamic_smem(smem_set, attn_paged_kernel<D, T>, S::SMEM) != DARE_OK) return DARE_ERR_CUDA;
+    return launch_kernel(attn_paged_kernel<D, T>, dim3(ctas), (PG_WARPS + 1) * 32, S::SMEM, stream, 1, tm_k, tm_v, p);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -704,7 +709,9 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     p.counters = ctx->join_counters; p.dev_status = ctx->dev_status;
     // two CTAs per SM, all resident at once; no more than there can be tiles
     const long long tiles = static_cast<long long>(B) * Hkv * ((static_cast<long long>(max_pages) * page_size + PG_KT - 1) / PG_KT);
-    if (tiles > (1LL << 29)) return DARE_ERR_SHAPE;
+    // Tiles are numbered in 32 bits, twice their count included, unless sequences that share their pages could have more of them: with 64 bits
+    // the divisions in front of a CTA's first tile take 1 sequence of 777 keys from 7.8 to 8.1 us, 64 of up to 4096 from 50.9 to 51.2.
+    const bool many = tiles > (1LL << 29);
     long long ctas = 2LL * ctx->sm_count;
     if (ctas > PAGED_MAX_CTAS) ctas = PAGED_MAX_CTAS;
     p.places = static_cast<int>(ctas);
@@ -720,5 +727,6 @@ extern "C" int dare_attn_paged(dare_ctx* ctx, int B, int L, int Hq, int Hkv, int
     if (rc == DARE_OK) rc = make_tmap_bf16_halves(ctx, &tm_v, v_pages, pool_rows, d, box_rows);
     if (rc != DARE_OK) return rc;
     const int n = static_cast<int>(ctas);
-    return d == 128 ? launch_paged<128>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64>(ctx, tm_k, tm_v, p, n, s);
+    if (many) return d == 128 ? launch_paged<128, int64_t>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64, int64_t>(ctx, tm_k, tm_v, p, n, s);
+    return d == 128 ? launch_paged<128, int>(ctx, tm_k, tm_v, p, n, s) : launch_paged<64, int>(ctx, tm_k, tm_v, p, n, s);
 }

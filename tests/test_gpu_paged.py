@@ -503,6 +503,34 @@ def test_attend_pool_beyond_32_bit_offsets(ctx):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("L,hq,hkv", [(1, 32, 32), (2, 128, 32), (3, 96, 32)])
+def test_attend_table_as_wide_as_allowed(ctx, L, hq, hkv):
+    """Two sequences, short, under a table of 2^30 positions: 2^34 of them and more over all KV heads."""
+    lens, page, d = [700, 3], 1024, 64
+    q, kp, vp, table = _attend_case(5, 2, L, hq, hkv, d, page, lens, 0, 0, plant=False)
+    wide = torch.full((2, 2 ** 30 // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = torch.from_numpy(table)
+    lse = torch.empty(2, hq, L, device="cuda")
+    out = dare.dare_attn_paged(ctx, q.cuda(), kp.cuda(), vp.cuda(), wide, torch.tensor(lens, dtype=torch.int32, device="cuda"), lse=lse)
+    assert ctx.device_status() == 0
+    _check_attend(out, lse, q, kp, vp, table, lens, 0, 0)
+
+
+def test_attend_many_sequences_under_a_wide_table(ctx):
+    """65536 sequences under 513 pages of 1024 positions: 2^29 + 2^20 tiles, if all were filled; the same as under 3."""
+    q = I.normal_bf16(6, 1, (65536, 1, 1, 64)).cuda()
+    kp, vp = (I.normal_bf16(6, 6 + i, (3, 1, 1024, 64)).cuda() for i in range(2))
+    lens = torch.from_numpy(np.random.default_rng(6).integers(0, 50, 65536).astype(np.int32))
+    lens[::5000] = 2 * 1024 + 77
+    table = torch.zeros(65536, 513, dtype=torch.int32, device="cuda")
+    table[:, :3] = torch.tensor([2, 0, 1], dtype=torch.int32)
+    lens = lens.cuda()
+    out = dare.dare_attn_paged(ctx, q, kp, vp, table, lens)
+    assert torch.equal(out, dare.dare_attn_paged(ctx, q, kp, vp, table[:, :3].contiguous(), lens)) and ctx.device_status() == 0
+    some = list(range(0, 65536, 5000)) + [65535]
+    _check_attend(out[some], None, q[some].cpu(), kp.cpu(), vp.cpu(), table[some, :3].cpu().numpy(), lens[some].tolist(), 0, 0)
+
+
 def _attend_on(ctx, q, kp, vp, table, lens, window=0, sinks=0):
     out = dare.dare_attn_paged(ctx, q, kp, vp, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), window=window, sinks=sinks)
     torch.cuda.synchronize()
