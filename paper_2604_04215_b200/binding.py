@@ -732,6 +732,12 @@ def _same(name: str, t, *shape):
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
 
 
+def _c_int(x) -> int:
+    """For ctypes, which would take an integer modulo 2^32: -1, which the library refuses, for one that is no C int >= 0."""
+    x = int(x)
+    return x if 0 <= x < 2 ** 31 else -1
+
+
 def _fused_heads(cols: int, n_kv_heads: int, d: int) -> int:
     """Query heads of a fused projection's row [(Hq + 2 Hkv) d]."""
     hq = cols // d - 2 * n_kv_heads
@@ -868,7 +874,7 @@ def dare_attn_paged(ctx: Context, q, k_pages, v_pages, block_table, kv_lens, win
         _same("lse", lse, B, hq, L)
         rc = load().dare_attn_paged(
             ctx.handle, B, L, hq, hkv, d, float(scale), _addr(q, bf, dev), _addr(k_pages, bf, dev), _addr(v_pages, bf, dev), n_pages, page,
-            _addr(block_table, i32, dev), block_table.shape[1], _addr(kv_lens, i32, dev), int(window), int(sinks), _addr(out, bf, dev),
+            _addr(block_table, i32, dev), block_table.shape[1], _addr(kv_lens, i32, dev), _c_int(window), _c_int(sinks), _addr(out, bf, dev),
             _addr(lse, torch.float32, dev), _stream(stream, dev))
     if rc != 0 and check:
         raise DareError(rc, "dare_attn_paged")

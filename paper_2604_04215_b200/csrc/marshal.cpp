@@ -185,7 +185,6 @@ PyObject* attn_paged_checked(PyObject* const* argv, Py_ssize_t n) {
     const long long window = a.integer(), sinks = a.integer();
     const at::Tensor *out = a.tensor(at::kBFloat16), *lse = a.tensor(at::kFloat);
     if (!a.ok || a.at != n || !q || !k || !v || !table || !lens || !out || q->dim() != 4 || k->dim() != 4 || table->dim() != 2) Py_RETURN_NONE;
-    if (window != static_cast<int>(window) || sinks != static_cast<int>(sinks)) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), Hq = q->size(2), d = q->size(3);
     if (k->size(3) != d || v->sizes() != k->sizes() || out->sizes() != q->sizes() || table->size(0) != B || !has_shape(lens, {B}) ||
         !has_shape(lse, {B, Hq, L}))
@@ -198,7 +197,7 @@ PyObject* attn_paged_checked(PyObject* const* argv, Py_ssize_t n) {
     int rc;
     Py_BEGIN_ALLOW_THREADS;
     rc = f_attn_paged(ctx, as_int(B), as_int(L), as_int(Hq), Hkv, as_int(d), scale, q_ptr, k_ptr, v_ptr, n_pages, page, t_ptr, max_pages, n_ptr,
-                      static_cast<int>(window), static_cast<int>(sinks), o_ptr, l_ptr, stream);
+                      as_int(window), as_int(sinks), o_ptr, l_ptr, stream);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(rc);
 }

@@ -704,6 +704,22 @@ def test_refusals(ctx):
         dare.dare_attn_paged(ctx, bf(2, 1, 4, 64), bf(5, 2, 16, 64), bf(5, 2, 16, 64), i32(2, 3), i32(2).long())
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_window_and_sinks_beyond_32_bits_are_refused(ctx, monkeypatch, native):
+    """Not taken modulo 2^32, by either way through the binding."""
+    if not native:
+        monkeypatch.setattr(dare, "_marshal", dare._NoNative)
+    q, pages = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
+    table, lens = torch.zeros(1, 2, dtype=torch.int32, device="cuda"), torch.full((1,), 20, dtype=torch.int32, device="cuda")
+    before = dare.dare_kernel_launches()
+    for kw in (dict(window=2 ** 32 + 5), dict(window=2 ** 31), dict(window=2 ** 70), dict(window=-2 ** 32 + 5), dict(window=5, sinks=2 ** 32),
+               dict(window=5, sinks=-2 ** 40)):
+        assert dare.dare_attn_paged(ctx, q, pages, pages, table, lens, check=False, **kw) == -4
+    assert dare.dare_kernel_launches() == before
+    dare.dare_attn_paged(ctx, q, pages, pages, table, lens, window=2 ** 31 - 1, sinks=2 ** 31 - 1)
+    assert dare.dare_kernel_launches() == before + 1 and ctx.device_status() == 0
+
+
 def test_workspace_too_small_is_refused():
     small = dare.Context(0, workspace_bytes=1 << 16)
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
