@@ -451,15 +451,20 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  * Norms of queries and keys per head, rotation, and a key-value cache in pages (rollouts of different lengths, prompts
  * shared by several rollouts, sequences that are not at the same position).  The stacks behind block-diffusion rollouts
  * (Section 3.4) normalise each query and key head before the rotation; dare_model_* does not, so these calls stand on
- * their own, around a caller's projections (dare_linear).
+ * their own, around a caller's projections (dare_linear).  What the library does not have next to them: a backward pass of an
+ * attention (d_q, d_k, d_v of dare_qk_norm_rope_backward come from the caller's), and a block-causal mask (several blocks of a known
+ * text in one call: one call of dare_attn_paged per block, each over the keys up to its end).
  *
  * dare_rope_table: table fp32 [n_positions, d/2, 2] = (cos, sin)(position * base^(-2c/d)), evaluated in 64 bits; laid out once.
+ *   d in {64, 128}, n_positions <= 2^24 (DARE_ERR_SHAPE), base > 1 and finite (DARE_ERR_RANGE).
  *
  * dare_qk_norm_rope: row m of qkv bf16 [n_rows, (Hq + 2 Hkv) d] (q heads, k heads, v heads) at position positions[m]:
  *     x <- x / sqrt(mean(x^2) + eps) * weight   for each q and k head (q_weight, k_weight bf16 [d]; both NULL: no norm)
  *     (x_c, x_{c+d/2}) <- (x_c cos - x_{c+d/2} sin, x_{c+d/2} cos + x_c sin)
  *   -> q_out bf16 [n_rows, Hq, d], k_out, v_out bf16 [n_rows, Hkv, d] (v copied); what dare_attn_varlen reads.  fp32 inside, rounded
- *   once.  A position outside [0, n_positions) gives zeros and sets DARE_DEV_INDEX_OUTSIDE.
+ *   once.  A position outside [0, n_positions) gives zeros and sets DARE_DEV_INDEX_OUTSIDE.  Here, in its backward pass and in
+ *   dare_paged_kv_append: Hq % Hkv == 0, d in {64, 128}, n_rows >= 1, n_rows * (Hq + 2 Hkv) <= 2^30 (DARE_ERR_SHAPE), eps >= 0 and finite
+ *   (DARE_ERR_RANGE).
  * dare_qk_norm_rope_backward: given the gradients d_q, d_k, d_v of those outputs, d_qkv bf16 (shape of qkv) and, with weights,
  *   d_q_weight, d_k_weight fp32 [d] (sums over all rows and heads in a fixed order; without weights ignored).  A row that the forward
  *   left at zero has a zero gradient.  Needs ctx workspace of 8 * d * (number of SMs) bytes with weights.
@@ -469,9 +474,9 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  * power of two from 16 to 1024; n_pages * Hkv * page_size < 2^31 - 1024; max_pages * page_size <= 2^30.
  *
  * dare_paged_kv_append: the arithmetic of dare_qk_norm_rope; q goes to q_out [n_rows, Hq, d], k and v to position positions[m] of
- *   sequence seq_ids[m].  A row with seq_ids[m] < 0 belongs to no sequence: nothing is read or written for it (a padded
- *   batch).  A sequence >= n_seqs, a position outside [0, min(n_positions, max_pages * page_size)) or a page outside [0, n_pages): the row is left
- *   out, q_out included, and DARE_DEV_INDEX_OUTSIDE is set.  Each position of the cache at most once per call.
+ *   sequence seq_ids[m].  A row with seq_ids[m] < 0 belongs to no sequence: what it holds does not matter and nothing is written
+ *   for it (a padded batch).  A sequence >= n_seqs, a position outside [0, min(n_positions, max_pages * page_size)) or a page outside
+ *   [0, n_pages): the row is left out, q_out included, and DARE_DEV_INDEX_OUTSIDE is set.  Each position of the cache at most once per call.
  *
  * dare_attn_paged: the last L positions of each sequence attend to it: n = kv_lens[b] keys, the L new ones (appended before)
  *   among them; query i of q bf16 [B, L, Hq, d] stands at position n - L + i.
@@ -481,9 +486,11 @@ int dare_generate_dual(dare_model* model, int32_t* tokens, int B, int64_t row_st
  *   (DARE_DEV_LEN_CLAMPED).  Pages that no query of the block can see, those between the sinks and the window and those
  *   behind n, are not read and their table entries may be anything; a page outside [0, n_pages) that one can see reads as zeros and
  *   sets DARE_DEV_INDEX_OUTSIDE.  Cached values that some query of a block sees must be finite for all of its queries.
- *   A query that is not finite has NaN in its own out and lse (where n > 0) and nowhere else.  Results do not depend on the order in which the GPU
- *   runs the parts.  Supported: Hq % Hkv == 0, Hq / Hkv <= 128, d in {64, 128}, L >= 1, L * Hq / Hkv <= 2^20, B * Hkv <= 65535 where
- *   that is more than 8; ctx workspace of 128 * (d + 2) bytes for each SM.
+ *   A query that is not finite has NaN in its own out and lse (where n > 0) and nowhere else.  Results do not depend on the order
+ *   in which the GPU runs the parts.  fp32 inside, out rounded once; with L * Hq / Hkv > 8 the weights are rounded to bf16 in front of
+ *   the second product too, as in dare_attn_block (out is then 2.3e-3 from 64 bits instead of 1.7e-3, 2-norm).  Supported: Hq % Hkv == 0,
+ *   Hq / Hkv <= 128, d in {64, 128}, L >= 1, L * Hq / Hkv <= 2^20, B * Hkv <= 65535 where that is more than 8; ctx workspace of
+ *   128 * (d + 2) bytes for each SM.
  *   n may be smaller than L (the positions of the first queries are then negative, the rule of what is visible stays).
  * Outputs of these calls do not overlap their inputs.
  */

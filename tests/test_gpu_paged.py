@@ -720,6 +720,29 @@ def test_window_and_sinks_beyond_32_bits_are_refused(ctx, monkeypatch, native):
     assert dare.dare_kernel_launches() == before + 1 and ctx.device_status() == 0
 
 
+def test_refusals_of_counts_beyond_the_limits(ctx):
+    """Given to the library as numbers: there is no memory for such tensors.  All are refused on the host."""
+    lib, hq, hkv, d = dare.load(), 4, 2, 64
+    x, pages = torch.zeros(4, 8 * d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, hkv, 16, d, dtype=torch.bfloat16, device="cuda")
+    ints, rope = torch.zeros(16, dtype=torch.int32, device="cuda"), torch.zeros(10, d // 2, 2, device="cuda")
+    a, i, r, pg = x.data_ptr(), ints.data_ptr(), rope.data_ptr(), pages.data_ptr()
+    before = dare.dare_kernel_launches()
+    rows = 2 ** 30 // (hq + 2 * hkv) + 1
+    assert lib.dare_qk_norm_rope(ctx.handle, a, rows, hq, hkv, d, None, None, EPS, i, r, 10, a, a, a, None) == -2
+    assert lib.dare_qk_norm_rope_backward(ctx.handle, a, rows, hq, hkv, d, None, None, EPS, i, r, 10, a, a, a, a, None, None, None) == -2
+    assert lib.dare_paged_kv_append(ctx.handle, a, rows, hq, hkv, d, None, None, EPS, r, 10, i, i, i, 1, 1, 1, 16, pg, pg, a, None) == -2
+    assert lib.dare_rope_table(ctx.handle, 2 ** 24 + 1, d, 10000.0, r, None) == -2
+    for base in (1.0, 0.5, 0.0, -2.0, float("inf"), float("nan")):
+        assert lib.dare_rope_table(ctx.handle, 10, d, base, r, None) == -4
+    for pool in ((2 ** 27, 16), (2 ** 21, 1024)):            # 2^31 rows of 2 KV heads and more: positions of the pool are 32-bit
+        n_pages, page = pool
+        assert lib.dare_attn_paged(ctx.handle, 1, 1, 4, 2, d, 0.0, a, pg, pg, n_pages, page, i, 1, i, 0, 0, a, None, None) == -2
+        assert lib.dare_paged_kv_append(ctx.handle, a, 1, hq, hkv, d, None, None, EPS, r, 10, i, i, i, 1, 1, n_pages, page, pg, pg, a, None) == -2
+    assert lib.dare_attn_paged(ctx.handle, 1, 1, 4, 2, d, 0.0, a, pg, pg, 1, 16, i, 2 ** 26 + 1, i, 0, 0, a, None, None) == -2
+    assert lib.dare_attn_paged(ctx.handle, 1, 2 ** 19 + 1, 4, 2, d, 0.0, a, pg, pg, 1, 16, i, 1, i, 0, 0, a, None, None) == -2
+    assert dare.dare_kernel_launches() == before and ctx.device_status() == 0
+
+
 def test_workspace_too_small_is_refused():
     small = dare.Context(0, workspace_bytes=1 << 16)
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
