@@ -988,7 +988,9 @@ attn_block_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             if (c + k < valid1) t0 = fmaxf(t0, __uint_as_float(v[k]));
                     }
                 }
-                const float tmax = fmaxf(t0, t1) * c2;     // log2 domain (the scale is > 0); finite: every tile has a key
+                const float tmax = fmaxf(t0, t1) * c2;     // log2 domain (the scale is > 0)
+                // (finite where every tile has a key for every row; PAGED: -inf in a tile that lies in front of this row's window and in an empty part,
+                // which neither moves the reference nor, while that is -inf too, weighs anything: nm = 0 below)
                 // move the reference only when the true max has run away from it (decided per warp, so that the
                 // TMEM loads and stores below are executed by whole warps; rows that are not live never ask for it, so that
                 // nobody's rounding depends on what lies behind the rollout or the sequence)
